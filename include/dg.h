@@ -217,6 +217,44 @@ dg_status_t dg_layer_bwd(dg_graph_t g, const float* dOut, const float* out, int3
                          float* G, float* dbias, void* stream);
 
 /*
+ * The graphs of a batch: one handle may hold the disjoint union of several graphs, one range of vertices each.
+ *   count    number of graphs; 0: one graph of all n vertices again (the state of a new handle; offsets is not read)
+ *   offsets  HOST, count + 1 entries, not decreasing, from 0 to at most n: graph b has the vertices offsets[b] ..
+ *            offsets[b + 1] - 1.  A graph may be empty; vertices from offsets[count] on belong to none (padding).
+ * Only the group norm below looks at them.  The handle keeps a copy on the device.  Waits for the whole device, like a
+ * change of "rows_per_block": CUDA graphs captured before it must not be launched afterwards.  If it fails the handle is
+ * as it was.  dg_graph_reorder does not carry the graphs over: it mixes their vertices.
+ */
+dg_status_t dg_graph_set_batch(dg_graph_t g, int64_t count, const int64_t* offsets);
+
+/*
+ * Group norm with an activation over vertex features, channels last: rows = the handle's vertices, the F columns in
+ * `groups` groups of F / groups neighbouring ones.  Mean and variance of a group are taken over its cells in all rows of
+ * one graph of the batch (dg_graph_set_batch; groups = 1: layer norm of a graph, groups = F: instance norm).
+ *
+ *   fwd:  rstd = 1 / sqrt(var + eps) with var the mean of (X - mean)^2;  hat = (X - mean) * rstd;
+ *         Y = act(hat * weight[f] + bias[f]);  stats[(b * groups + c) * 2] = mean, [... + 1] = rstd of graph b, group c
+ *         (an empty graph: 0 and 1 / sqrt(eps)).
+ *   bwd:  d = dY * act'(hat * weight + bias);  dbias[f] = sum of d, dweight[f] = sum of d * hat over all graphs' rows;
+ *         dX = rstd * (d * weight - A - hat * B), A and B the means of d * weight and of d * weight * hat of the group.
+ *   X, dX    device, n x F row-major of x_type;  Y, dY  device, n x F of y_type
+ *   weight, bias  device, F fp32 each, or NULL: 1 and 0
+ *   stats    device, graphs * groups * 2 fp32, 8-byte aligned; written by fwd, read by bwd
+ *   dX, dweight, dbias  each may be NULL and is not formed then
+ * Statistics and sums are fp32 or wider and always added in the same order; a result is rounded to its type once.  Rows that belong to no
+ * graph are neither read nor written.  Results must not overlap inputs.  The ReLU's gradient is that of z > 0 with the
+ * sign of z taken in 64 bits where fp32 leaves it open.  graphs * groups < 2^31.  Asynchronous on `stream`.
+ */
+typedef enum { DG_F32 = 0, DG_BF16 = 1 } dg_type_t;
+typedef enum { DG_ACT_NONE = 0, DG_ACT_RELU = 1, DG_ACT_SILU = 2 } dg_act_t;
+dg_status_t dg_group_norm_fwd(dg_graph_t g, const void* X, dg_type_t x_type, int32_t F, int32_t groups,
+                              const float* weight, const float* bias, float eps, dg_act_t act, void* Y,
+                              dg_type_t y_type, float* stats, void* stream);
+dg_status_t dg_group_norm_bwd(dg_graph_t g, const void* dY, dg_type_t y_type, const void* X, dg_type_t x_type, int32_t F,
+                              int32_t groups, const float* weight, const float* bias, const float* stats, dg_act_t act,
+                              void* dX, float* dweight, float* dbias, void* stream);
+
+/*
  * The matrix products of such a layer on fp32 matrices, X n x K, W N x K, G n x N (n = the handle's vertices),
  * to fp32 accuracy on the tensor cores: for all finite numbers the 2-norm errors of sums of sixteen numbers (that are not 0)
  * and more are below those of the same sum in fp32 arithmetic, term by term; of fewer up to 1.8 times those.

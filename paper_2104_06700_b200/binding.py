@@ -25,12 +25,15 @@ DG_OP_MEAN = 1
 DG_BIN_COPY_LHS, DG_BIN_COPY_RHS, DG_BIN_ADD, DG_BIN_SUB, DG_BIN_MUL, DG_BIN_DIV = range(6)
 DG_RED_SUM, DG_RED_MAX, DG_RED_MIN = range(3)
 DG_ORDER_GIVEN, DG_ORDER_OUT_DEGREE, DG_ORDER_IN_DEGREE = range(3)
+DG_F32, DG_BF16 = range(2)
+DG_ACT_NONE, DG_ACT_RELU, DG_ACT_SILU = range(3)
 
 EXPORTS = [
     "dg_graph_create", "dg_graph_destroy", "dg_graph_validate", "dg_graph_transpose_workspace",
     "dg_graph_transpose", "dg_graph_transpose_static", "dg_graph_update_weights", "dg_graph_get_csc", "dg_aggregate_fwd", "dg_aggregate_bwd",
     "dg_aggregate_fwd_self", "dg_aggregate_bwd_self", "dg_layer_fwd", "dg_layer_bwd",
     "dg_linear_fwd", "dg_linear_bwd_input", "dg_linear_bwd_weight",
+    "dg_graph_set_batch", "dg_group_norm_fwd", "dg_group_norm_bwd",
     "dg_cross_entropy_fwd", "dg_cross_entropy_bwd",
     "dg_aggregate_fwd_bf16", "dg_aggregate_bwd_bf16",
     "dg_ap_fwd", "dg_ap_bwd", "dg_aggregate_edge_grad",
@@ -78,6 +81,10 @@ def lib() -> ctypes.CDLL:
         L.dg_linear_fwd.argtypes = [p, p, i32, p, i32, p, p, i32, p, p]
         L.dg_linear_bwd_input.argtypes = [p, p, i32, p, i32, p, p]
         L.dg_linear_bwd_weight.argtypes = [p, p, i32, p, i32, p, p]
+        L.dg_graph_set_batch.argtypes = [p, i64, p]
+        f32, enum = ctypes.c_float, ctypes.c_int
+        L.dg_group_norm_fwd.argtypes = [p, p, enum, i32, i32, p, p, f32, enum, p, enum, p, p]
+        L.dg_group_norm_bwd.argtypes = [p, p, enum, p, enum, i32, i32, p, p, p, enum, p, p, p, p]
         L.dg_cross_entropy_fwd.argtypes = [p, p, i32, p, i64, p, p, p, p]
         L.dg_cross_entropy_bwd.argtypes = [p, p, i32, p, i64, p, p, p, p, p, p]
         L.dg_aggregate_fwd_bf16.argtypes = [p, p, i32, ctypes.c_int, p, p]
@@ -139,6 +146,24 @@ def _is_matrix(t: torch.Tensor, rows: int, columns: int, name: str) -> None:
 def _has(t: Optional[torch.Tensor], count: int, name: str) -> None:
     if t is not None and t.numel() != count:
         raise ValueError(f"{name} must have {count} values, got {t.numel()}")
+
+
+_TYPE_CODES = {torch.float32: DG_F32, torch.bfloat16: DG_BF16}
+
+
+def _typed_ptr(t: torch.Tensor, name: str):
+    """(device pointer, dg_type_t) of an fp32 or bf16 tensor."""
+    code = _TYPE_CODES.get(t.dtype)
+    if code is None:
+        raise TypeError(f"{name} must be torch.float32 or torch.bfloat16, got {t.dtype}")
+    return _dev_ptr(t, t.dtype, name), code
+
+
+def _on_current_device(**tensors) -> None:
+    """A call's kernels run on the current device: every tensor has to be there."""
+    for name, t in tensors.items():
+        if t is not None and t.is_cuda and t.get_device() != _device():
+            raise ValueError(f"{name} is on {t.device}, the current device is cuda:{_device()}")
 
 
 # The handle of the current stream of the current device.  torch.cuda.current_stream() builds two
@@ -213,6 +238,7 @@ class Graph:
         self.rowptr, self.colidx, self.edge_w = rowptr, colidx, edge_w
         self._csc = None
         self._storage = None
+        self.batch = None       # host copy of the offsets given to dg_graph_set_batch
         if _adopt is not None:          # a handle the library made (dg_graph_reorder)
             self._h, self._storage = _adopt
             return
@@ -431,6 +457,90 @@ class Graph:
                                           _dev_ptr(X, torch.float32, "X"), K, _dev_ptr(dW, torch.float32, "dW"),
                                           _stream(stream)))
         return dW
+
+    def dg_graph_set_batch(self, offsets) -> None:
+        """``offsets``: vertex offsets of the graphs (a sequence or an int64 tensor, count + 1 entries), or None for one
+        graph of all vertices."""
+        if offsets is None:
+            _check(lib().dg_graph_set_batch(self._h, 0, None))
+            self.batch = None
+            return
+        given = torch.as_tensor(offsets)
+        if given.is_floating_point() or given.dtype == torch.bool or given.dim() != 1 or given.numel() < 2:
+            raise ValueError("offsets must be at least two whole numbers")
+        host = given.to("cpu", torch.int64).contiguous()
+        _check(lib().dg_graph_set_batch(self._h, host.numel() - 1, host.data_ptr()))
+        self.batch = host.clone()
+
+    def _norm_shapes(self, F, groups, weight, bias, **matrices):
+        """(graphs, rows that belong to a graph)"""
+        for name, t in matrices.items():
+            if t is not None:
+                _is_matrix(t, self.n, F, name)
+        if groups < 1 or F % groups:
+            raise ValueError(f"groups must divide {F}, got {groups}")
+        _has(weight, F, "weight")
+        _has(bias, F, "bias")
+        _on_current_device(weight=weight, bias=bias, **matrices)
+        return (1, self.n) if self.batch is None else (self.batch.numel() - 1, int(self.batch[-1]))
+
+    def _result(self, X, dtype, rows, stream):
+        """A matrix like X, zeros in the rows behind `rows`: written on the stream that the call goes to."""
+        out = torch.empty(X.shape, dtype=dtype, device=X.device)
+        if rows < self.n:
+            if stream is None:
+                out[rows:].zero_()
+            else:
+                with torch.cuda.stream(stream):
+                    out[rows:].zero_()
+        return out
+
+    def dg_group_norm_fwd(self, X: torch.Tensor, groups: int, weight: Optional[torch.Tensor] = None,
+                          bias: Optional[torch.Tensor] = None, eps: float = 1e-5, act: int = DG_ACT_NONE,
+                          Y: Optional[torch.Tensor] = None, y_dtype=None, stats: Optional[torch.Tensor] = None,
+                          stream=None):
+        """(Y, stats) of the group norm with an activation; stats is (graphs, groups, 2): mean and 1 / sqrt(var + eps).
+        Without ``Y`` a matrix of ``y_dtype`` (X's) is made, with zeros in the rows that belong to no graph; in a given one
+        they stay as they are."""
+        F = X.shape[1]
+        graphs, rows = self._norm_shapes(F, groups, weight, bias, X=X, Y=Y)
+        if Y is None:
+            Y = self._result(X, y_dtype or X.dtype, rows, stream)
+        elif y_dtype is not None and y_dtype != Y.dtype:
+            raise TypeError(f"Y is {Y.dtype}, not {y_dtype}")
+        if stats is None:
+            stats = torch.empty((graphs, groups, 2), dtype=torch.float32, device=X.device)
+        _has(stats, graphs * groups * 2, "stats")
+        _on_current_device(stats=stats)
+        (x, x_type), (y, y_type) = _typed_ptr(X, "X"), _typed_ptr(Y, "Y")
+        _check(lib().dg_group_norm_fwd(self._h, x, x_type, F, int(groups), _dev_ptr(weight, torch.float32, "weight"),
+                                       _dev_ptr(bias, torch.float32, "bias"), float(eps), int(act), y, y_type,
+                                       _dev_ptr(stats, torch.float32, "stats"), _stream(stream)))
+        return Y, stats
+
+    def dg_group_norm_bwd(self, dY: torch.Tensor, X: torch.Tensor, stats: torch.Tensor, groups: int,
+                          weight: Optional[torch.Tensor] = None, bias: Optional[torch.Tensor] = None,
+                          act: int = DG_ACT_NONE, dX: Optional[torch.Tensor] = None, want_dX: bool = True,
+                          want_dweight: bool = True, want_dbias: bool = True, stream=None):
+        """(dX, dweight, dbias), each None where it is not wanted.  Rows that belong to no graph: as in the forward call."""
+        F = X.shape[1]
+        graphs, rows = self._norm_shapes(F, groups, weight, bias, X=X, dY=dY, dX=dX)
+        _has(stats, graphs * groups * 2, "stats")
+        _on_current_device(stats=stats)
+        if dX is None and want_dX:
+            dX = self._result(X, X.dtype, rows, stream)
+        elif dX is not None and dX.dtype != X.dtype:
+            raise TypeError(f"dX must be {X.dtype}, got {dX.dtype}")
+        dweight = X.new_empty(F, dtype=torch.float32) if want_dweight else None
+        dbias = X.new_empty(F, dtype=torch.float32) if want_dbias else None
+        (x, x_type), (dy, y_type) = _typed_ptr(X, "X"), _typed_ptr(dY, "dY")
+        _check(lib().dg_group_norm_bwd(self._h, dy, y_type, x, x_type, F, int(groups),
+                                       _dev_ptr(weight, torch.float32, "weight"), _dev_ptr(bias, torch.float32, "bias"),
+                                       _dev_ptr(stats, torch.float32, "stats"), int(act),
+                                       None if dX is None else _typed_ptr(dX, "dX")[0],
+                                       None if dweight is None else dweight.data_ptr(),
+                                       None if dbias is None else dbias.data_ptr(), _stream(stream)))
+        return dX, dweight, dbias
 
     def _loss_shapes(self, logits, index, labels) -> None:
         _holds(logits, self.n * logits.shape[1], "logits")

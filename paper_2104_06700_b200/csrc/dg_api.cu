@@ -8,6 +8,7 @@
 #include <new>
 
 #include "dg_internal.cuh"
+#include "dg_norm.cuh"
 
 namespace dg {
 
@@ -45,6 +46,7 @@ static inline size_t align256(size_t x) { return (x + 255) & ~(size_t)255; }
 static void free_owned(Graph* g) {
   pool_retire(g->device, g->owned, g->owned_bytes);
   pool_retire(g->device, g->plan_memory, g->plan_bytes);
+  pool_retire(g->device, g->batch_memory, g->batch_bytes);
   pinned_counters_retire(g->device, g->host);
   if (g->col_totals_ready) cudaEventDestroy(g->col_totals_ready);
   for (size_t i = 0; i < g->aux_event_count; ++i) cudaEventDestroy(g->aux_events[i]);
@@ -458,6 +460,100 @@ dg_status_t dg_layer_bwd(dg_graph_t g, const float* dOut, const float* out, int3
   if (F < 1 || F > (1 << 20)) return invalid("F must be from 1 to 2^20");
   if (!dbias || (g->n > 0 && (!dOut || !row_scale || !G))) return invalid("a pointer is NULL");
   return layer_bwd(g, dOut, out, F, row_scale, G, dbias, (cudaStream_t)stream);
+}
+
+dg_status_t dg_graph_set_batch(dg_graph_t g, int64_t count, const int64_t* offsets) {
+  if (!g) return invalid("graph handle is NULL");
+  if (count < 0 || count >= ((int64_t)1 << 31)) return invalid("count must be from 0 to 2^31 - 1");
+  if (count > 0 && !offsets) return invalid("offsets is NULL");
+  int64_t longest = 0;
+  if (count > 0 && offsets[0] != 0) return invalid("offsets[0] must be 0");
+  for (int64_t b = 0; b < count; ++b) {
+    const int64_t rows = offsets[b + 1] - offsets[b];
+    if (offsets[b + 1] < offsets[b] || offsets[b + 1] > g->n) return invalid("offsets must not decrease or pass n");
+    if (rows > longest) longest = rows;
+  }
+  const DeviceScope scope(g->device);
+  const size_t bytes = count > 0 ? align256((size_t)(count + 1) * sizeof(int64_t)) : 0;
+  void* memory = nullptr;
+  if (count > 0) {
+    DG_CUDA(pool_wait(g->device));
+    DG_CUDA(pool_alloc(g->device, bytes, 0, &memory));
+    cudaError_t e = cudaMemcpyAsync(memory, offsets, (size_t)(count + 1) * sizeof(int64_t), cudaMemcpyHostToDevice, 0);
+    if (e == cudaSuccess) e = cudaStreamSynchronize(0);
+    if (e != cudaSuccess) {
+      pool_retire(g->device, memory, bytes);
+      return cuda_fail(e, "dg_graph_set_batch");
+    }
+  }
+  pool_retire(g->device, g->batch_memory, g->batch_bytes);
+  g->batch_memory = memory;
+  g->batch_bytes = bytes;
+  g->batch_offsets = static_cast<const int64_t*>(memory);
+  g->batch_count = count > 0 ? count : 1;
+  g->batch_rows = count > 0 ? offsets[count] : -1;
+  g->batch_longest = count > 0 ? longest : -1;
+  return DG_OK;
+}
+
+// The arguments that both directions share, checked; a->out and a->dY are the caller's.
+static dg_status_t norm_args(const Graph* g, const void* X, dg_type_t x_type, int32_t F, int32_t groups,
+                             const float* weight, const float* bias, const float* stats, dg_act_t act, dg_type_t y_type,
+                             NormArgs* a) {
+  if (!g) return invalid("graph handle is NULL");
+  if (F < 1 || F > (1 << 20)) return invalid("F must be from 1 to 2^20");
+  if (groups < 1 || groups > F || F % groups != 0) return invalid("groups must divide F");
+  if ((x_type != DG_F32 && x_type != DG_BF16) || (y_type != DG_F32 && y_type != DG_BF16))
+    return invalid("a type must be DG_F32 or DG_BF16");
+  if (act != DG_ACT_NONE && act != DG_ACT_RELU && act != DG_ACT_SILU) return invalid("unknown activation");
+  if (g->batch_count * groups >= ((int64_t)1 << 31)) {
+    set_error("graphs x groups must be below 2^31");
+    return DG_ERR_UNSUPPORTED;
+  }
+  if (!stats || (g->n > 0 && !X)) return invalid("a pointer is NULL");
+  if ((uintptr_t)stats & 7) return invalid("stats must be 8-byte aligned");
+  if ((uintptr_t)X % (x_type == DG_F32 ? 4 : 2)) return invalid("X must be aligned to its type");
+  a->X = X;
+  a->stats = reinterpret_cast<float2*>(const_cast<float*>(stats));
+  a->weight = weight;
+  a->bias = bias;
+  a->offsets = g->batch_offsets;
+  a->rows = g->batch_rows < 0 ? g->n : g->batch_rows;
+  a->graphs = g->batch_count;
+  a->F = F;
+  a->groups = groups;
+  a->width = F / groups;
+  return DG_OK;
+}
+
+dg_status_t dg_group_norm_fwd(dg_graph_t g, const void* X, dg_type_t x_type, int32_t F, int32_t groups,
+                              const float* weight, const float* bias, float eps, dg_act_t act, void* Y,
+                              dg_type_t y_type, float* stats, void* stream) {
+  NormArgs a{};
+  if (dg_status_t st = norm_args(g, X, x_type, F, groups, weight, bias, stats, act, y_type, &a)) return st;
+  if (!(eps >= 0.f)) return invalid("eps must not be negative");
+  if (g->n > 0 && !Y) return invalid("a pointer is NULL");
+  const size_t cells = (size_t)g->n * (size_t)F, x_size = x_type == DG_F32 ? 4 : 2, y_size = y_type == DG_F32 ? 4 : 2;
+  if ((uintptr_t)Y % y_size) return invalid("Y must be aligned to its type");
+  if (overlaps(X, cells * x_size, Y, cells * y_size)) return invalid("the result overlaps an input");
+  a.out = Y;
+  a.eps = eps;
+  return group_norm_fwd(g, a, x_type, y_type, act, (cudaStream_t)stream);
+}
+
+dg_status_t dg_group_norm_bwd(dg_graph_t g, const void* dY, dg_type_t y_type, const void* X, dg_type_t x_type, int32_t F,
+                              int32_t groups, const float* weight, const float* bias, const float* stats, dg_act_t act,
+                              void* dX, float* dweight, float* dbias, void* stream) {
+  NormArgs a{};
+  if (dg_status_t st = norm_args(g, X, x_type, F, groups, weight, bias, stats, act, y_type, &a)) return st;
+  if (g->n > 0 && !dY) return invalid("a pointer is NULL");
+  const size_t cells = (size_t)g->n * (size_t)F, x_size = x_type == DG_F32 ? 4 : 2, y_size = y_type == DG_F32 ? 4 : 2;
+  if ((uintptr_t)dY % y_size || (uintptr_t)dX % x_size) return invalid("dY and dX must be aligned to their types");
+  if (dX && (overlaps(X, cells * x_size, dX, cells * x_size) || overlaps(dY, cells * y_size, dX, cells * x_size)))
+    return invalid("the result overlaps an input");
+  a.dY = dY;
+  a.out = g->n > 0 ? dX : nullptr;
+  return group_norm_bwd(g, a, x_type, y_type, act, dweight, dbias, (cudaStream_t)stream);
 }
 
 // The inputs a and b and the result, with their numbers of elements.

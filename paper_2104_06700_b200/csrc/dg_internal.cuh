@@ -90,6 +90,14 @@ struct dg_graph {
   const int32_t* new_of_old = nullptr;   // n: new id of every old vertex
   const int32_t* reorder_pos = nullptr;  // nnz: old CSR position of every new position
 
+  // the graphs of a batch (dg_graph_set_batch): graph b has the rows batch_offsets[b] .. batch_offsets[b + 1]
+  void* batch_memory = nullptr;  // owned
+  size_t batch_bytes = 0;
+  const int64_t* batch_offsets = nullptr;  // device; nullptr: one graph of all rows
+  int64_t batch_count = 1;
+  int64_t batch_rows = -1;       // behind the last graph's last row; -1: n
+  int64_t batch_longest = -1;    // rows of the longest graph; -1: n
+
   int device = 0;
   int sm_count = 148;
   size_t l2_bytes = 0;
