@@ -9,6 +9,7 @@ from __future__ import annotations
 
 import ctypes
 import os
+import struct
 from typing import Optional
 
 import torch
@@ -33,6 +34,7 @@ EXPORTS = [
     "dg_graph_transpose", "dg_graph_transpose_static", "dg_graph_update_weights", "dg_graph_get_csc", "dg_aggregate_fwd", "dg_aggregate_bwd",
     "dg_aggregate_fwd_self", "dg_aggregate_bwd_self", "dg_layer_fwd", "dg_layer_bwd",
     "dg_linear_fwd", "dg_linear_bwd_input", "dg_linear_bwd_weight",
+    "dg_grad_norm", "dg_adamw_step",
     "dg_graph_set_batch", "dg_group_norm_fwd", "dg_group_norm_bwd",
     "dg_cross_entropy_fwd", "dg_cross_entropy_bwd",
     "dg_aggregate_fwd_bf16", "dg_aggregate_bwd_bf16",
@@ -85,6 +87,9 @@ def lib() -> ctypes.CDLL:
         f32, enum = ctypes.c_float, ctypes.c_int
         L.dg_group_norm_fwd.argtypes = [p, p, enum, i32, i32, p, p, f32, enum, p, enum, p, p]
         L.dg_group_norm_bwd.argtypes = [p, p, enum, p, enum, i32, i32, p, p, p, enum, p, p, p, p]
+        f64 = ctypes.c_double
+        L.dg_grad_norm.argtypes = [i64, p, f32, p, p, p]
+        L.dg_adamw_step.argtypes = [i64, p, f64, f64, f64, f64, f64, p, ctypes.c_uint64, p, p]
         L.dg_cross_entropy_fwd.argtypes = [p, p, i32, p, i64, p, p, p, p]
         L.dg_cross_entropy_bwd.argtypes = [p, p, i32, p, i64, p, p, p, p, p, p]
         L.dg_aggregate_fwd_bf16.argtypes = [p, p, i32, ctypes.c_int, p, p]
@@ -227,6 +232,82 @@ def dg_permute_rows(new_of_old: torch.Tensor, x: torch.Tensor, to_old: bool = Fa
                                  _dev_ptr(out, torch.float32, "out"), int(bool(to_old)),
                                  _stream(stream)))
     return out
+
+
+DG_ADAMW_WORKSPACE_BYTES = 8192
+_adamw_tensor = struct.Struct("7Qq3iI").pack      # dg_adamw_tensor_t
+
+
+def _checked(t: torch.Tensor, dtypes, count: int, device: int, name: str) -> int:
+    if t.dtype not in dtypes:
+        raise TypeError(f"{name} must be {' or '.join(map(str, dtypes))}, got {t.dtype}")
+    if t.get_device() != device:
+        raise ValueError(f"{name} must be on cuda:{device}, it is on {t.device}")
+    if not t.is_contiguous():
+        raise ValueError(f"{name} must be contiguous")
+    if t.numel() != count:
+        raise ValueError(f"{name} must have {count} values, got {t.numel()}")
+    return t.data_ptr()
+
+
+_FLOATS = (torch.float32, torch.bfloat16)
+_E4M3, _F32_ONLY, _I64, _BF16 = (torch.float8_e4m3fn,), (torch.float32,), (torch.int64,), (torch.bfloat16,)
+
+
+def adamw_tensor(param: torch.Tensor, grad: torch.Tensor, exp_avg: torch.Tensor, exp_avg_sq: torch.Tensor,
+                 step: torch.Tensor, scales: Optional[torch.Tensor] = None, copy: Optional[torch.Tensor] = None,
+                 id: int = 0) -> bytes:
+    """A ``dg_adamw_tensor_t`` for the two calls below, which take a list of them.  The states are fp32, or float8_e4m3fn with
+    ``scales``; everything is contiguous, on one device, and has to live until the call."""
+    count, device = param.numel(), param.get_device()
+    if device < 0:
+        raise ValueError("param must be a CUDA tensor")
+    p = _checked(param, _FLOATS, count, device, "param")
+    g = _checked(grad, _FLOATS, count, device, "grad")
+    states = _F32_ONLY if scales is None else _E4M3
+    return _adamw_tensor(
+        p, g, _checked(exp_avg, states, count, device, "exp_avg"), _checked(exp_avg_sq, states, count, device, "exp_avg_sq"),
+        0 if scales is None else _checked(scales, _F32_ONLY, 2 * ((count + 255) // 256), device, "scales"),
+        0 if copy is None else _checked(copy, _BF16, count, device, "copy"), _checked(step, _I64, 1, device, "step"), count,
+        _TYPE_CODES[param.dtype], _TYPE_CODES[grad.dtype], 32 if scales is None else 8, id)
+
+
+def gradient_tensor(grad: torch.Tensor) -> bytes:
+    """A ``dg_adamw_tensor_t`` of a gradient alone, for ``dg_grad_norm``."""
+    if not grad.is_cuda:
+        raise ValueError("grad must be a CUDA tensor")
+    g = _checked(grad, _FLOATS, grad.numel(), grad.get_device(), "grad")
+    return _adamw_tensor(0, g, 0, 0, 0, 0, 0, grad.numel(), 0, _TYPE_CODES[grad.dtype], 0, 0)
+
+
+def adamw_workspace(device) -> torch.Tensor:
+    """The workspace of the two calls: cleared once, then theirs."""
+    return torch.zeros(DG_ADAMW_WORKSPACE_BYTES, dtype=torch.uint8, device=device)
+
+
+def _workspace_ptr(workspace):
+    _has(workspace, DG_ADAMW_WORKSPACE_BYTES, "workspace")
+    _on_current_device(workspace=workspace)
+    return _dev_ptr(workspace, torch.uint8, "workspace")
+
+
+def dg_grad_norm(tensors: list, max_norm: float, workspace: torch.Tensor, result: torch.Tensor, stream=None) -> torch.Tensor:
+    """Wraps ``dg_grad_norm``: result (2 fp32) = (norm of all gradients, min(1, max_norm / (norm + 1e-6)))."""
+    _has(result, 2, "result")
+    _on_current_device(result=result)
+    _check(lib().dg_grad_norm(len(tensors), b"".join(tensors), float(max_norm), _workspace_ptr(workspace),
+                              _dev_ptr(result, torch.float32, "result"), _stream(stream)))
+    return result
+
+
+def dg_adamw_step(tensors: list, lr: float, beta1: float, beta2: float, eps: float, weight_decay: float,
+                  workspace: torch.Tensor, grad_factor: Optional[torch.Tensor] = None, seed: int = 0, stream=None) -> None:
+    """Wraps ``dg_adamw_step``: updates the tensors, their states and their steps in place."""
+    _has(grad_factor, 1, "grad_factor")
+    _on_current_device(grad_factor=grad_factor)
+    _check(lib().dg_adamw_step(len(tensors), b"".join(tensors), lr, beta1, beta2, eps, weight_decay,
+                               _dev_ptr(grad_factor, torch.float32, "grad_factor"), seed & 0xffffffffffffffff,
+                               _workspace_ptr(workspace), _stream(stream)))
 
 
 class Graph:

@@ -1,0 +1,144 @@
+"""AdamW over all parameters in one launch, its states in 32 or 8 bits, with clipping by the norm of all gradients
+(dg_adamw_step and dg_grad_norm), behind torch's optimiser interface."""
+from __future__ import annotations
+
+from typing import Optional
+
+import torch
+
+from . import binding
+
+
+class AdamW(torch.optim.Optimizer):
+    """torch.optim.AdamW's update (decoupled weight decay) for fp32 and bf16 parameters on one GPU.
+
+    ``state_bits``: 8 keeps the averages of tensors of ``min_8bit_size`` numbers and more in e4m3 with a scale for every
+    256 (2.03 bytes a number instead of 8); they are rounded up or down at random, by a hash of ``seed``, the step and the place.
+    ``master_weights``: bf16 parameters get fp32 master weights in the state and are their roundings.  Without them a bf16
+    parameter itself is rounded at random, so that small steps are not lost.
+    ``max_norm``: gradients are scaled as clip_grad_norm_ would (the norm is that of all groups' gradients together); they are
+    left as they are.  ``grad_norm`` is the last step's, a tensor of one number that the next step overwrites.
+
+    A parameter's state: ``step`` (int64, on the device: a step can be captured into a CUDA graph once it has run outside one),
+    ``exp_avg``, ``exp_avg_sq`` (with 8 bits the square root of it, and ``scales`` (blocks, 2) of both), ``master``.  lr and the
+    other options are taken by value: a captured step repeats them.
+    """
+
+    def __init__(self, params, lr: float = 1e-3, betas=(0.9, 0.999), eps: float = 1e-8, weight_decay: float = 1e-2,
+                 state_bits: int = 32, min_8bit_size: int = 4096, master_weights: bool = False,
+                 max_norm: Optional[float] = None, seed: int = 0):
+        if state_bits not in (8, 32):
+            raise ValueError(f"state_bits must be 8 or 32, got {state_bits}")
+        if max_norm is not None and not max_norm > 0:
+            raise ValueError(f"max_norm must be positive, got {max_norm}")
+        if not lr >= 0 or not eps >= 0 or not weight_decay >= 0:
+            raise ValueError("lr, eps and weight_decay must not be negative")
+        if len(betas) != 2 or not all(0 <= b < 1 for b in betas):
+            raise ValueError(f"betas must be in [0, 1), got {betas}")
+        self.max_norm, self.grad_norm = max_norm, None
+        self._workspace = self._result = None
+        super().__init__(params, dict(lr=lr, betas=betas, eps=eps, weight_decay=weight_decay, state_bits=state_bits,
+                                      min_8bit_size=min_8bit_size, master_weights=master_weights, seed=seed))
+
+    def add_param_group(self, group) -> None:
+        super().add_param_group(group)
+        params = self.param_groups[-1]["params"]
+        if len(set(params)) != len(params):
+            raise ValueError("a parameter stands in its group twice: the one launch would update it twice at once")
+
+    def __getstate__(self):     # workspaces are not state
+        state = super().__getstate__()
+        return {**state, "max_norm": self.max_norm}
+
+    def __setstate__(self, state) -> None:
+        super().__setstate__(state)
+        self.__dict__.setdefault("max_norm", None)
+        self.grad_norm = self._workspace = self._result = None
+
+    def load_state_dict(self, state_dict) -> None:
+        """torch's would cast every state to its parameter's type."""
+        super().load_state_dict(state_dict)
+        saved = state_dict["state"]
+        params = [p for group in self.param_groups for p in group["params"]]
+        numbers = [i for group in state_dict["param_groups"] for i in group["params"]]
+        for i, p in zip(numbers, params):
+            if i in saved:
+                self.state[p] = {k: v.detach().to(p.device, copy=True).contiguous() if torch.is_tensor(v) else v
+                                 for k, v in saved[i].items()}
+
+    def _new_state(self, p: torch.Tensor, group) -> dict:
+        if not p.is_cuda or p.dtype not in (torch.float32, torch.bfloat16) or not p.is_contiguous():
+            raise ValueError("parameters must be contiguous fp32 or bf16 CUDA tensors")
+        if torch.cuda.is_current_stream_capturing():
+            raise RuntimeError("run a step before capturing one: a captured first step would begin anew at every replay")
+        eight = group["state_bits"] == 8 and p.numel() >= group["min_8bit_size"]
+        dtype = torch.float8_e4m3fn if eight else torch.float32
+        state = {"step": torch.zeros((), dtype=torch.int64, device=p.device),
+                 "exp_avg": torch.zeros(p.shape, dtype=torch.float32, device=p.device).to(dtype),
+                 "exp_avg_sq": torch.zeros(p.shape, dtype=torch.float32, device=p.device).to(dtype)}
+        if eight:
+            state["scales"] = torch.zeros(((p.numel() + 255) // 256, 2), dtype=torch.float32, device=p.device)
+        if group["master_weights"] and p.dtype == torch.bfloat16:
+            state["master"] = p.detach().float()
+        return state
+
+    def _tensors(self, group, first: int) -> list:
+        """The group's tensors for the library; the random bits of the i-th go by first + i."""
+        tensors = []
+        for i, p in enumerate(group["params"], first):
+            g = p.grad
+            if g is None:
+                continue
+            if g.is_sparse:
+                raise ValueError("sparse gradients are not supported")
+            if self._device is None:
+                self._device = p.device
+            elif p.device != self._device:
+                raise ValueError(f"parameters are on {self._device} and on {p.device}: one step runs on one device")
+            s = self.state[p]
+            if not s:
+                s.update(self._new_state(p, group))
+            if not g.is_contiguous():
+                g = g.contiguous()
+                self._kept.append(g)        # until the launch is queued; the allocator's stream order does the rest
+            master = s.get("master")
+            target, copy = (p, None) if master is None else (master, p)
+            tensors.append(binding.adamw_tensor(target, g, s["exp_avg"], s["exp_avg_sq"], s["step"], s.get("scales"), copy, i))
+        return tensors
+
+    @torch.no_grad()
+    def step(self, closure=None):
+        loss = None
+        if closure is not None:
+            with torch.enable_grad():
+                loss = closure()
+        self._kept, self._device, lists, first = [], None, [], 0
+        for group in self.param_groups:
+            lists.append(self._tensors(group, first))
+            first += len(group["params"])
+        every = [t for tensors in lists for t in tensors]
+        if every:
+            if self._device.index == torch.cuda.current_device():
+                self._launch(lists, every)
+            else:
+                with torch.cuda.device(self._device):
+                    self._launch(lists, every)
+        self._kept = []
+        return loss
+
+    def _launch(self, lists, every) -> None:
+        device = self._device
+        if self._workspace is None or self._workspace.device != device:
+            if torch.cuda.is_current_stream_capturing():
+                raise RuntimeError("run a step before capturing one")
+            self._workspace = binding.adamw_workspace(device)
+            self._result = torch.zeros(2, dtype=torch.float32, device=device)
+        factor = None
+        if self.max_norm is not None:
+            binding.dg_grad_norm(every, self.max_norm, self._workspace, self._result)
+            self.grad_norm, factor = self._result[0], self._result[1]
+        for group, tensors in zip(self.param_groups, lists):
+            if tensors:
+                beta1, beta2 = group["betas"]
+                binding.dg_adamw_step(tensors, group["lr"], beta1, beta2, group["eps"], group["weight_decay"], self._workspace,
+                                      factor, group["seed"])
