@@ -462,6 +462,8 @@ dg_status_t dg_layer_bwd(dg_graph_t g, const float* dOut, const float* out, int3
   return layer_bwd(g, dOut, out, F, row_scale, G, dbias, (cudaStream_t)stream);
 }
 
+static int64_t offsets_end(int64_t count, const int64_t* offsets) { return count > 0 ? offsets[count] : 0; }
+
 dg_status_t dg_graph_set_batch(dg_graph_t g, int64_t count, const int64_t* offsets) {
   if (!g) return invalid("graph handle is NULL");
   if (count < 0 || count >= ((int64_t)1 << 31)) return invalid("count must be from 0 to 2^31 - 1");
@@ -474,22 +476,49 @@ dg_status_t dg_graph_set_batch(dg_graph_t g, int64_t count, const int64_t* offse
     if (rows > longest) longest = rows;
   }
   const DeviceScope scope(g->device);
-  const size_t bytes = count > 0 ? align256((size_t)(count + 1) * sizeof(int64_t)) : 0;
-  void* memory = nullptr;
+  // pieces of at least 64 rows, and enough of them for every SM to have several
+  int64_t rows = (offsets_end(count, offsets) + g->sm_count * 16 - 1) / (g->sm_count * 16);
+  if (rows < 64) rows = 64;
+  int64_t pieces = 0;
+  for (int64_t b = 0; b < count; ++b) pieces += (offsets[b + 1] - offsets[b] + rows - 1) / rows;
+  const size_t offset_bytes = align256((size_t)(count + 1) * sizeof(int64_t));
+  const size_t first_bytes = align256((size_t)(count + 1) * sizeof(int32_t));
+  const size_t bytes = offset_bytes + first_bytes + align256((size_t)pieces * sizeof(Piece));
+  char* memory = nullptr;
   if (count > 0) {
-    DG_CUDA(pool_wait(g->device));
-    DG_CUDA(pool_alloc(g->device, bytes, 0, &memory));
-    cudaError_t e = cudaMemcpyAsync(memory, offsets, (size_t)(count + 1) * sizeof(int64_t), cudaMemcpyHostToDevice, 0);
+    char* host = static_cast<char*>(malloc(bytes));
+    if (!host) return invalid("out of host memory");
+    memcpy(host, offsets, (size_t)(count + 1) * sizeof(int64_t));
+    int32_t* first = reinterpret_cast<int32_t*>(host + offset_bytes);
+    Piece* piece = reinterpret_cast<Piece*>(host + offset_bytes + first_bytes);
+    int32_t made = 0;
+    for (int64_t b = 0; b < count; ++b) {
+      first[b] = made;
+      for (int64_t row = offsets[b]; row < offsets[b + 1]; row += rows) {
+        const int64_t left = offsets[b + 1] - row;
+        piece[made++] = Piece{(int32_t)b, (int32_t)row, (int32_t)(left < rows ? left : rows), 0};
+      }
+    }
+    first[count] = made;
+    void* block = nullptr;
+    cudaError_t e = pool_wait(g->device);
+    if (e == cudaSuccess) e = pool_alloc(g->device, bytes, 0, &block);
+    if (e == cudaSuccess) e = cudaMemcpyAsync(block, host, bytes, cudaMemcpyHostToDevice, 0);
     if (e == cudaSuccess) e = cudaStreamSynchronize(0);
+    free(host);
     if (e != cudaSuccess) {
-      pool_retire(g->device, memory, bytes);
+      pool_retire(g->device, block, bytes);
       return cuda_fail(e, "dg_graph_set_batch");
     }
+    memory = static_cast<char*>(block);
   }
   pool_retire(g->device, g->batch_memory, g->batch_bytes);
   g->batch_memory = memory;
-  g->batch_bytes = bytes;
-  g->batch_offsets = static_cast<const int64_t*>(memory);
+  g->batch_bytes = memory ? bytes : 0;
+  g->batch_offsets = reinterpret_cast<const int64_t*>(memory);
+  g->batch_first = memory ? reinterpret_cast<const int32_t*>(memory + offset_bytes) : nullptr;
+  g->batch_pieces = memory ? reinterpret_cast<const Piece*>(memory + offset_bytes + first_bytes) : nullptr;
+  g->batch_piece_count = (int32_t)pieces;
   g->batch_count = count > 0 ? count : 1;
   g->batch_rows = count > 0 ? offsets[count] : -1;
   g->batch_longest = count > 0 ? longest : -1;

@@ -10,6 +10,8 @@
 
 namespace dg {
 
+struct Piece;
+
 // One warp's share of a pass over the CSR rows (or CSC columns): the entries [pos, next chunk's
 // pos), which belong to the rows from `row` up to the next chunk's row.  Chunks hold about the same
 // number of entries.  They begin at row starts, except inside rows longer than the split threshold:
@@ -94,6 +96,9 @@ struct dg_graph {
   void* batch_memory = nullptr;  // owned
   size_t batch_bytes = 0;
   const int64_t* batch_offsets = nullptr;  // device; nullptr: one graph of all rows
+  const dg::Piece* batch_pieces = nullptr;  // device: the graphs cut into runs of rows, in order
+  const int32_t* batch_first = nullptr;     // device, batch_count + 1: the first piece of every graph
+  int32_t batch_piece_count = 0;
   int64_t batch_count = 1;
   int64_t batch_rows = -1;       // behind the last graph's last row; -1: n
   int64_t batch_longest = -1;    // rows of the longest graph; -1: n

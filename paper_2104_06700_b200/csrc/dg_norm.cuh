@@ -9,6 +9,8 @@
 
 #include <cuda_bf16.h>
 
+#include <type_traits>
+
 #include "dg_internal.cuh"
 
 namespace dg {
@@ -72,7 +74,157 @@ __device__ __forceinline__ float before_activation(float dy, float x, float mean
   return dy * (s * fmaf(z, 1.f - s, 1.f));
 }
 
-// dg_norm.cu
+// ---- rows in pieces: the kernels of long graphs ------------------------------------------------------------------
+
+// A run of rows of one graph, for one block (and one tile of channels).
+struct Piece {
+  int32_t graph, row, rows, pad;
+};
+
+// How a matrix is shared out.  Threads lie along the vectors of a tile of channels first (`across`), then along the rows
+// (`down`); a thread keeps to its channels.
+struct NormShape {
+  int32_t vec;       // channels of a vector
+  int32_t across, down, tiles;
+  int32_t rows;      // of a piece where one graph has all rows
+  int32_t pieces;
+};
+
+constexpr int kNormThreads = 256;
+
+// VEC neighbouring numbers as fp32.
+template <int VEC>
+struct Channels {
+  float v[VEC];
+};
+template <typename T, int VEC>
+__device__ __forceinline__ Channels<VEC> load_channels(const T* p) {
+  Channels<VEC> r;
+  if constexpr (sizeof(T) == 4 && VEC == 4) {
+    const float4 q = *reinterpret_cast<const float4*>(p);
+    r.v[0] = q.x, r.v[1] = q.y, r.v[2] = q.z, r.v[3] = q.w;
+  } else if constexpr (sizeof(T) == 4 && VEC == 2) {
+    const float2 q = *reinterpret_cast<const float2*>(p);
+    r.v[0] = q.x, r.v[1] = q.y;
+  } else if constexpr (sizeof(T) == 2 && VEC >= 2) {
+    uint32_t w[VEC / 2];
+    if constexpr (VEC == 8) {
+      const uint4 q = *reinterpret_cast<const uint4*>(p);
+      w[0] = q.x, w[1] = q.y, w[2] = q.z, w[3] = q.w;
+    } else if constexpr (VEC == 4) {
+      const uint2 q = *reinterpret_cast<const uint2*>(p);
+      w[0] = q.x, w[1] = q.y;
+    } else {
+      w[0] = *reinterpret_cast<const uint32_t*>(p);
+    }
+#pragma unroll
+    for (int i = 0; i < VEC / 2; ++i) {
+      r.v[2 * i] = __uint_as_float(w[i] << 16);
+      r.v[2 * i + 1] = __uint_as_float(w[i] & 0xffff0000u);
+    }
+  } else {
+    static_assert(VEC == 1, "one number");
+    r.v[0] = as_float(*p);
+  }
+  return r;
+}
+template <typename T, int VEC>
+__device__ __forceinline__ void store_channels(T* p, const Channels<VEC>& r) {
+  if constexpr (sizeof(T) == 4 && VEC == 4) {
+    __stcs(reinterpret_cast<float4*>(p), make_float4(r.v[0], r.v[1], r.v[2], r.v[3]));
+  } else if constexpr (sizeof(T) == 4 && VEC == 2) {
+    __stcs(reinterpret_cast<float2*>(p), make_float2(r.v[0], r.v[1]));
+  } else if constexpr (sizeof(T) == 2 && VEC >= 2) {
+    uint32_t w[VEC / 2];
+#pragma unroll
+    for (int i = 0; i < VEC / 2; ++i) {
+      const __nv_bfloat162 pair = __floats2bfloat162_rn(r.v[2 * i], r.v[2 * i + 1]);
+      w[i] = *reinterpret_cast<const uint32_t*>(&pair);
+    }
+    if constexpr (VEC == 8)
+      __stcs(reinterpret_cast<uint4*>(p), make_uint4(w[0], w[1], w[2], w[3]));
+    else if constexpr (VEC == 4)
+      __stcs(reinterpret_cast<uint2*>(p), make_uint2(w[0], w[1]));
+    else
+      __stcs(reinterpret_cast<unsigned int*>(p), w[0]);
+  } else {
+    static_assert(VEC == 1, "one number");
+    *p = as<T>(r.v[0]);
+  }
+}
+
+// Where a thread works: its piece, its first channel, its place along the rows.
+struct Place {
+  Piece piece;
+  int32_t channel;   // >= F: none
+  int32_t y, down;
+};
+__device__ __forceinline__ Place place_of(const NormArgs& a, const NormShape& sh, const Piece* pieces, int32_t p) {
+  Place r;
+  if (pieces) {
+    r.piece = pieces[p];
+  } else {
+    const int64_t row = (int64_t)p * sh.rows, left = a.rows - row;
+    r.piece = Piece{0, (int32_t)row, (int32_t)(left < sh.rows ? left : sh.rows), 0};
+  }
+  r.y = threadIdx.x / sh.across;
+  r.down = sh.down;
+  const int32_t vector = blockIdx.y * sh.across + threadIdx.x % sh.across;
+  r.channel = r.y < sh.down && vector < a.F / sh.vec ? vector * sh.vec : a.F;
+  return r;
+}
+
+// How a call's matrices are shared out among blocks.
+NormShape norm_shape(const Graph* g, const NormArgs& a, int vec);
+// The widest vectors that rows of F numbers and these pointers allow.
+int norm_vector(const NormArgs& a, dg_type_t x, dg_type_t y);
+
+// f(X, Y, act) for the call's types and activation
+template <typename Fn>
+dg_status_t by_type(dg_type_t x, dg_type_t y, dg_act_t act, Fn f) {
+  auto with_act = [&](auto xs, auto ys) {
+    if (act == DG_ACT_RELU) return f(xs, ys, std::integral_constant<int, DG_ACT_RELU>());
+    if (act == DG_ACT_SILU) return f(xs, ys, std::integral_constant<int, DG_ACT_SILU>());
+    return f(xs, ys, std::integral_constant<int, DG_ACT_NONE>());
+  };
+  if (x == DG_F32) return y == DG_F32 ? with_act(float(), float()) : with_act(float(), __nv_bfloat16());
+  return y == DG_F32 ? with_act(__nv_bfloat16(), float()) : with_act(__nv_bfloat16(), __nv_bfloat16());
+}
+// f(VEC): 8 for two bf16 matrices alone
+template <bool WIDE, typename Fn>
+auto by_vector(int vec, Fn f) {
+  if constexpr (WIDE)
+    if (vec == 8) return f(std::integral_constant<int, 8>());
+  if (vec == 4) return f(std::integral_constant<int, 4>());
+  if (vec == 2) return f(std::integral_constant<int, 2>());
+  return f(std::integral_constant<int, 1>());
+}
+
+// The sum of v over a block of at most 1024 threads, in every thread and always in the same order.
+__device__ __forceinline__ double block_sum(double v) {
+  __shared__ double sums[32];
+#pragma unroll
+  for (int o = 16; o > 0; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
+  if (blockDim.x == 32) return v;
+  __syncthreads();  // the last call's sums have been read
+  if (threadIdx.x % 32 == 0) sums[threadIdx.x / 32] = v;
+  __syncthreads();
+  v = 0.0;
+  for (int i = 0; i < (int)blockDim.x / 32; ++i) v += sums[i];
+  return v;
+}
+
+// ---- one block for a group, where a call has no scratch ---------------------------------------------------------
+
+// Calls f(index of the cell, its channel) for the thread's cells of a group.  Threads lie along the channels first.
+template <typename Fn>
+__device__ __forceinline__ void for_cells(const NormArgs& a, Rows r, int32_t channel, int across, Fn f) {
+  const int x = threadIdx.x % across, y = threadIdx.x / across, down = kNormThreads / across;
+  for (int64_t row = r.lo + y; row < r.hi; row += down)
+    for (int32_t c = x; c < a.width; c += across) f(row * a.F + channel + c, channel + c);
+}
+
+// dg_norm.cu, dg_norm_bwd.cu
 dg_status_t group_norm_fwd(const Graph* g, const NormArgs& a, dg_type_t x, dg_type_t y, dg_act_t act, cudaStream_t s);
 dg_status_t group_norm_bwd(const Graph* g, const NormArgs& a, dg_type_t x, dg_type_t y, dg_act_t act, float* dweight,
                            float* dbias, cudaStream_t s);

@@ -3,9 +3,10 @@ import torch
 
 U = 2.0 ** -24                      # half a step of fp32, relative
 HALF_STEP = {torch.float32: U, torch.bfloat16: 2.0 ** -8}
-# Roundings on the way of a number into a sum, at the sizes tested: at most 16 rows in registers, 4 for each join of two
-# parts of a thread (at most 16) and of a block's threads (at most 9 levels), and one at the end.
-CHAIN = 16 + 4 * (16 + 9) + 1
+# Roundings on the way of a number into a sum, at the sizes tested: a thread adds at most 8 rows of 8 channels in
+# registers, 4 for each join of two parts of a thread (at most 16) and of a block's threads (at most 9 levels), and one at
+# the end.
+CHAIN = 8 * 8 + 4 * (16 + 9) + 1
 
 
 def activation(z, act):
