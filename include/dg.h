@@ -293,26 +293,31 @@ dg_status_t dg_cross_entropy_bwd(dg_graph_t g, const float* logits, int32_t C, c
                                  const float* result, const float* grad, float* dLogits, void* stream);
 
 /*
- * AdamW over many tensors in one launch (one per 400 of them), and the norm of all gradients.  With t = the tensor's steps so far + 1:
+ * AdamW over many tensors in one launch (one per 400 of them), and the norm of all gradients.  With
+ * t = the tensor's steps so far + 1:
  *
  *   g = grad * factor;  m = m + (1 - beta1) * (g - m);  v = beta2 * v + (1 - beta2) * g * g;
  *   param = param * (1 - lr * weight_decay) - lr / (1 - beta1^t) * m / (sqrt(v) / sqrt(1 - beta2^t) + eps)
  *
- *   param       device, count fp32 or bf16 (param_type), updated in place.  A bf16 parameter is rounded up or down at random (see seed)
- *   copy        device, count bf16 that receive the new values of an fp32 param, rounded to nearest (param: the master weights
- *               of a bf16 model), or NULL
- *   grad        device, count fp32 or bf16 (grad_type), read only
- *   exp_avg, exp_avg_sq  device: state_bits = 32: m and v, count fp32 each.  state_bits = 8: m and sqrt(v), count e4m3 bytes
- *               each, times the scales; rounded up or down at random, a sqrt(v) > 0 never to 0.  A number that is not finite
- *               becomes NaN and leaves the rest of its block alone
- *   scales      state_bits = 8: device, 2 fp32 for every 256 numbers begun (of m, of sqrt(v)), 8-byte aligned
- *   step        device, steps taken so far; read, then increased by 1 by the call (one number for each tensor)
- *   id          what the random bits of the tensor go by, beside the seed
- * All zeros are the states of a new tensor.  Tensors must not overlap; each is contiguous, in any alignment to its type.
+ * A list names `tensors` tensors by HOST arrays of that many entries (the device pointers in them have to live until the kernels
+ * have run, the arrays until the call returns).  For tensor i:
+ *   numbers     how many numbers it has; each array of it is contiguous, in any alignment to its type
+ *   param       fp32 or bf16 (param_type), updated in place.  A bf16 parameter is rounded up or down at random (see seed)
+ *   copy        bf16 numbers that receive the new values of an fp32 param, rounded to nearest (param: the master weights of a
+ *               bf16 model), or NULL; the array itself may be NULL
+ *   grad        fp32 or bf16 (grad_type), read only
+ *   exp_avg, exp_avg_sq  state_bits = 32: m and v, fp32.  state_bits = 8: m and sqrt(v), e4m3 bytes, times the scales; rounded
+ *               up or down at random, a sqrt(v) > 0 never to 0.  A number that is not finite becomes NaN and leaves the rest
+ *               of its block alone
+ *   scales      state_bits = 8: 2 fp32 for every 256 numbers begun (of m, of sqrt(v)), 8-byte aligned; else NULL, and the array
+ *               itself may be NULL where all are
+ *   step        steps taken so far; read, then increased by 1 by the call (one number for each tensor)
+ *   id          what the random bits of the tensor go by, beside the seed; the array may be NULL: i
+ * All zeros are the states of a new tensor.  Tensors must not overlap.
  * dg_adamw_step: `grad_factor` is a device fp32 or NULL (1): result + 1 of dg_grad_norm.  The random bits of a rounding are a hash
  * of (seed, steps so far, id, place): the same call on the same data gives the same bits.  lr and the others are taken by
  * value: a captured call repeats them, while the steps go on counting.
- * dg_grad_norm: result[0] = the 2-norm of all gradients (only grad, grad_type and count of a tensor are looked at), added in 64
+ * dg_grad_norm: result[0] = the 2-norm of all gradients (of a list only grad, grad_type and numbers are looked at), added in 64
  * bits in a fixed order, result[1] = min(1, max_norm / (result[0] + 1e-6)): clipping by the norm.
  *   workspace   device, DG_ADAMW_WORKSPACE_BYTES, 256-byte aligned, cleared to 0 before its first use; calls leave it ready for
  *               the next.  Calls that may run at the same time need one each
@@ -320,23 +325,23 @@ dg_status_t dg_cross_entropy_bwd(dg_graph_t g, const float* logits, int32_t C, c
  */
 #define DG_ADAMW_WORKSPACE_BYTES 8192
 typedef struct {
-  void* param;
-  const void* grad;
-  void* exp_avg;
-  void* exp_avg_sq;
-  float* scales;
-  void* copy;
-  int64_t* step;
-  int64_t count;
-  int32_t param_type, grad_type; /* dg_type_t */
-  int32_t state_bits;
-  uint32_t id;
-} dg_adamw_tensor_t;
-dg_status_t dg_grad_norm(int64_t count, const dg_adamw_tensor_t* tensors, float max_norm, void* workspace,
-                         float* result, void* stream);
-dg_status_t dg_adamw_step(int64_t count, const dg_adamw_tensor_t* tensors, double lr, double beta1, double beta2,
-                          double eps, double weight_decay, const float* grad_factor, uint64_t seed, void* workspace,
-                          void* stream);
+  int64_t tensors;
+  const int64_t* numbers;
+  void* const* param;
+  const void* const* grad;
+  void* const* exp_avg;
+  void* const* exp_avg_sq;
+  float* const* scales;
+  void* const* copy;
+  int64_t* const* step;
+  const int32_t* param_type; /* dg_type_t */
+  const int32_t* grad_type;
+  const int32_t* state_bits;
+  const uint32_t* id;
+} dg_adamw_list_t;
+dg_status_t dg_grad_norm(const dg_adamw_list_t* list, float max_norm, void* workspace, float* result, void* stream);
+dg_status_t dg_adamw_step(const dg_adamw_list_t* list, double lr, double beta1, double beta2, double eps,
+                          double weight_decay, const float* grad_factor, uint64_t seed, void* workspace, void* stream);
 
 /*
  * dg_aggregate_fwd / dg_aggregate_bwd with the gathered matrix stored as bf16 (two bytes per element, the

@@ -10,6 +10,7 @@ from __future__ import annotations
 import ctypes
 import os
 import struct
+from array import array
 from typing import Optional
 
 import torch
@@ -88,8 +89,8 @@ def lib() -> ctypes.CDLL:
         L.dg_group_norm_fwd.argtypes = [p, p, enum, i32, i32, p, p, f32, enum, p, enum, p, p]
         L.dg_group_norm_bwd.argtypes = [p, p, enum, p, enum, i32, i32, p, p, p, enum, p, p, p, p]
         f64 = ctypes.c_double
-        L.dg_grad_norm.argtypes = [i64, p, f32, p, p, p]
-        L.dg_adamw_step.argtypes = [i64, p, f64, f64, f64, f64, f64, p, ctypes.c_uint64, p, p]
+        L.dg_grad_norm.argtypes = [p, f32, p, p, p]
+        L.dg_adamw_step.argtypes = [p, f64, f64, f64, f64, f64, p, ctypes.c_uint64, p, p]
         L.dg_cross_entropy_fwd.argtypes = [p, p, i32, p, i64, p, p, p, p]
         L.dg_cross_entropy_bwd.argtypes = [p, p, i32, p, i64, p, p, p, p, p, p]
         L.dg_aggregate_fwd_bf16.argtypes = [p, p, i32, ctypes.c_int, p, p]
@@ -235,53 +236,84 @@ def dg_permute_rows(new_of_old: torch.Tensor, x: torch.Tensor, to_old: bool = Fa
 
 
 DG_ADAMW_WORKSPACE_BYTES = 8192
-_adamw_tensor = struct.Struct("7Qq3iI").pack      # dg_adamw_tensor_t
-
-
-def _checked(t: torch.Tensor, dtypes, count: int, device: int, name: str) -> int:
-    if t.dtype not in dtypes:
-        raise TypeError(f"{name} must be {' or '.join(map(str, dtypes))}, got {t.dtype}")
-    if t.get_device() != device:
-        raise ValueError(f"{name} must be on cuda:{device}, it is on {t.device}")
-    if not t.is_contiguous():
-        raise ValueError(f"{name} must be contiguous")
-    if t.numel() != count:
-        raise ValueError(f"{name} must have {count} values, got {t.numel()}")
-    return t.data_ptr()
-
-
 _FLOATS = (torch.float32, torch.bfloat16)
-_E4M3, _F32_ONLY, _I64, _BF16 = (torch.float8_e4m3fn,), (torch.float32,), (torch.int64,), (torch.bfloat16,)
+_data_ptr, _numel, _contiguous = torch.Tensor.data_ptr, torch.Tensor.numel, torch.Tensor.is_contiguous
+_get_device, _dtype = torch.Tensor.get_device, torch.Tensor.dtype.__get__
 
 
-def adamw_tensor(param: torch.Tensor, grad: torch.Tensor, exp_avg: torch.Tensor, exp_avg_sq: torch.Tensor,
-                 step: torch.Tensor, scales: Optional[torch.Tensor] = None, copy: Optional[torch.Tensor] = None,
-                 id: int = 0) -> bytes:
-    """A ``dg_adamw_tensor_t`` for the two calls below, which take a list of them.  The states are fp32, or float8_e4m3fn with
-    ``scales``; everything is contiguous, on one device, and has to live until the call."""
-    count, device = param.numel(), param.get_device()
-    if device < 0:
-        raise ValueError("param must be a CUDA tensor")
-    p = _checked(param, _FLOATS, count, device, "param")
-    g = _checked(grad, _FLOATS, count, device, "grad")
-    states = _F32_ONLY if scales is None else _E4M3
-    return _adamw_tensor(
-        p, g, _checked(exp_avg, states, count, device, "exp_avg"), _checked(exp_avg_sq, states, count, device, "exp_avg_sq"),
-        0 if scales is None else _checked(scales, _F32_ONLY, 2 * ((count + 255) // 256), device, "scales"),
-        0 if copy is None else _checked(copy, _BF16, count, device, "copy"), _checked(step, _I64, 1, device, "step"), count,
-        _TYPE_CODES[param.dtype], _TYPE_CODES[grad.dtype], 32 if scales is None else 8, id)
+def _check_tensors(tensors, dtypes, device: int, name: str) -> None:
+    """All contiguous, on one device and of one of the types.  The calls take long lists: whole ones are asked, tensor by
+    tensor only to say which one is wrong."""
+    if (device >= 0 and set(map(_dtype, tensors)) <= dtypes and set(map(_get_device, tensors)) <= {device} and all(map(_contiguous, tensors))):
+        return
+    for i, t in enumerate(tensors):
+        if t.dtype not in dtypes:
+            raise TypeError(f"{name}[{i}] must be {' or '.join(sorted(map(str, dtypes)))}, got {t.dtype}")
+        if t.get_device() != device or device < 0:
+            raise ValueError(f"{name}[{i}] must be a CUDA tensor on the current device, it is on {t.device}")
+        if not t.is_contiguous():
+            raise ValueError(f"{name}[{i}] must be contiguous")
 
 
-def gradient_tensor(grad: torch.Tensor) -> bytes:
-    """A ``dg_adamw_tensor_t`` of a gradient alone, for ``dg_grad_norm``."""
-    if not grad.is_cuda:
-        raise ValueError("grad must be a CUDA tensor")
-    g = _checked(grad, _FLOATS, grad.numel(), grad.get_device(), "grad")
-    return _adamw_tensor(0, g, 0, 0, 0, 0, 0, grad.numel(), 0, _TYPE_CODES[grad.dtype], 0, 0)
+def _check_sizes(tensors, numbers, name: str) -> None:
+    got = list(map(_numel, tensors))
+    if got != numbers:
+        raise ValueError(f"{name} must hold {numbers} values, got {got}")
+
+
+def _pointers(tensors) -> array:
+    return array("Q", map(_data_ptr, tensors))
+
+
+def _codes(tensors) -> array:
+    return array("i", map(_TYPE_CODES.__getitem__, map(_dtype, tensors)))
+
+
+class AdamwList:
+    """A ``dg_adamw_list_t``: parameters with their gradients, states and steps, in lists of one length.  ``scales[i]`` is a
+    tensor where the states of parameter i are 8-bit (float8_e4m3fn) and None where they are fp32; ``copies[i]`` a bf16 copy
+    of an fp32 parameter or None.  With gradients alone it serves ``dg_grad_norm``."""
+
+    def __init__(self, grads, params=None, exp_avgs=None, exp_avg_sqs=None, steps=None, scales=None, copies=None, ids=None):
+        self.count = len(grads)
+        self._keep = grads      # what a caller made for this list alone has to live until the launch
+        device = _device() if self.count and grads[0].is_cuda else -1
+        _check_tensors(grads, set(_FLOATS), device, "grads")
+        numbers = list(map(_numel, grads))
+        grad_types, grad_pointers = _codes(grads), _pointers(grads)
+        fields = [array("q", numbers), None, grad_pointers, None, None, None, None, None, None, grad_types, None, None]
+        if params is not None:
+            for name, tensors, types in (("params", params, set(_FLOATS)), ("steps", steps, {torch.int64})):
+                _check_tensors(tensors, types, device, name)
+            _check_sizes(params, numbers, "params")
+            _check_sizes(steps, [1] * self.count, "steps")
+            eight = [s is not None for s in scales] if scales is not None else [False] * self.count
+            for name, tensors in (("exp_avgs", exp_avgs), ("exp_avg_sqs", exp_avg_sqs)):
+                _check_sizes(tensors, numbers, name)
+                _check_tensors([t for t, e in zip(tensors, eight) if e], {torch.float8_e4m3fn}, device, name)
+                _check_tensors([t for t, e in zip(tensors, eight) if not e], {torch.float32}, device, name)
+            fields[1], fields[3:5], fields[7] = _pointers(params), map(_pointers, (exp_avgs, exp_avg_sqs)), _pointers(steps)
+            fields[8] = _codes(params)
+            fields[10] = array("i", [8 if e else 32 for e in eight])
+            fields[11] = array("I", range(self.count) if ids is None else ids)
+            if len(fields[11]) != self.count:
+                raise ValueError("ids must be as many as the tensors")
+            if any(eight):
+                some = [s for s in scales if s is not None]
+                _check_tensors(some, {torch.float32}, device, "scales")
+                _check_sizes(some, [2 * ((n + 255) // 256) for n, e in zip(numbers, eight) if e], "scales")
+                fields[5] = array("Q", [0 if s is None else s.data_ptr() for s in scales])
+            if copies is not None and any(c is not None for c in copies):
+                some = [c for c in copies if c is not None]
+                _check_tensors(some, {torch.bfloat16}, device, "copies")
+                _check_sizes(some, [n for n, c in zip(numbers, copies) if c is not None], "copies")
+                fields[6] = array("Q", [0 if c is None else c.data_ptr() for c in copies])
+        self._fields = fields
+        self.struct = struct.pack("q12Q", self.count, *[0 if f is None else f.buffer_info()[0] for f in fields])
 
 
 def adamw_workspace(device) -> torch.Tensor:
-    """The workspace of the two calls: cleared once, then theirs."""
+    """The workspace of the two calls below: cleared once, then theirs."""
     return torch.zeros(DG_ADAMW_WORKSPACE_BYTES, dtype=torch.uint8, device=device)
 
 
@@ -291,21 +323,21 @@ def _workspace_ptr(workspace):
     return _dev_ptr(workspace, torch.uint8, "workspace")
 
 
-def dg_grad_norm(tensors: list, max_norm: float, workspace: torch.Tensor, result: torch.Tensor, stream=None) -> torch.Tensor:
+def dg_grad_norm(tensors: AdamwList, max_norm: float, workspace: torch.Tensor, result: torch.Tensor, stream=None) -> torch.Tensor:
     """Wraps ``dg_grad_norm``: result (2 fp32) = (norm of all gradients, min(1, max_norm / (norm + 1e-6)))."""
     _has(result, 2, "result")
     _on_current_device(result=result)
-    _check(lib().dg_grad_norm(len(tensors), b"".join(tensors), float(max_norm), _workspace_ptr(workspace),
+    _check(lib().dg_grad_norm(tensors.struct, float(max_norm), _workspace_ptr(workspace),
                               _dev_ptr(result, torch.float32, "result"), _stream(stream)))
     return result
 
 
-def dg_adamw_step(tensors: list, lr: float, beta1: float, beta2: float, eps: float, weight_decay: float,
+def dg_adamw_step(tensors: AdamwList, lr: float, beta1: float, beta2: float, eps: float, weight_decay: float,
                   workspace: torch.Tensor, grad_factor: Optional[torch.Tensor] = None, seed: int = 0, stream=None) -> None:
     """Wraps ``dg_adamw_step``: updates the tensors, their states and their steps in place."""
     _has(grad_factor, 1, "grad_factor")
     _on_current_device(grad_factor=grad_factor)
-    _check(lib().dg_adamw_step(len(tensors), b"".join(tensors), lr, beta1, beta2, eps, weight_decay,
+    _check(lib().dg_adamw_step(tensors.struct, lr, beta1, beta2, eps, weight_decay,
                                _dev_ptr(grad_factor, torch.float32, "grad_factor"), seed & 0xffffffffffffffff,
                                _workspace_ptr(workspace), _stream(stream)))
 

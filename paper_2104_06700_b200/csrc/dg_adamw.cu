@@ -15,13 +15,14 @@ namespace {
 
 constexpr int kThreads = 256;
 constexpr int kWarps = kThreads / 32;
+constexpr int kBlocksPerSm = 3;                     // what 80 registers a thread leave room for
 constexpr int kNumbers = 256;                       // of a warp's task: 8 a lane, and one scale
 constexpr int kNormBlocks = 148 * 4;
 constexpr float kLargest = 448.f;                   // of e4m3
 constexpr float kLeastScale = 0x1p-126f;            // its inverse is finite
 
 // What a launch is told of its tensors, by value: at most 32764 bytes of arguments.
-constexpr int kMost = 400;
+constexpr int kMost = 400, kFew = 24;
 enum { kParamBf16 = 1, kGradBf16 = 2, k8Bits = 4, kVectors = 8 };
 template <int N>
 struct Tensors {
@@ -164,6 +165,12 @@ __device__ __forceinline__ float warp_max(float v) {
   for (int o = 16; o > 0; o >>= 1) v = fmaxf(v, __shfl_xor_sync(0xffffffffu, v, o));
   return v;
 }
+// off by at most 2^-23 of itself
+__device__ __forceinline__ float fast_sqrt(float v) {
+  float r;
+  asm("sqrt.approx.f32 %0, %1;" : "=f"(r) : "f"(v));
+  return r;
+}
 // the largest of the finite ones: a number that is not finite keeps to itself
 __device__ __forceinline__ float finite_max(float m, float v) { return v < INFINITY ? fmaxf(m, v) : m; }
 
@@ -208,8 +215,8 @@ __device__ __forceinline__ void update(const Tensors<N>& a, int i, int64_t base,
     const float gj = g[j] * factor;
     m[j] = fmaf(h.rest1, gj - m[j], m[j]);
     v[j] = fmaf(h.rest2 * gj, gj, h.beta2 * v[j]);
-    u[j] = sqrtf(v[j]);
-    p[j] = fmaf(p[j], h.decay, -st.c1 * (m[j] / fmaf(u[j], st.c2, h.eps)));
+    u[j] = fast_sqrt(v[j]);
+    p[j] = fmaf(p[j], h.decay, -st.c1 * __fdividef(m[j], fmaf(u[j], st.c2, h.eps)));
     if (EIGHT) {
       most_m = finite_max(most_m, fabsf(m[j]));
       most_u = finite_max(most_u, u[j]);
@@ -269,17 +276,25 @@ __device__ __forceinline__ void update(const Tensors<N>& a, int i, int64_t base,
 template <int N, typename P, typename G>
 __device__ __forceinline__ void update_typed(const Tensors<N>& a, int i, int64_t base, const Hyper& h, const Step& st,
                                              float factor) {
+  const bool vectors = a.flags[i] & kVectors && base + kNumbers <= a.count[i];
   if (a.flags[i] & k8Bits) {
-    update<N, P, G, true, false>(a, i, base, h, st, factor);
+    if (vectors)
+      update<N, P, G, true, true>(a, i, base, h, st, factor);
+    else
+      update<N, P, G, true, false>(a, i, base, h, st, factor);
   } else {
-    update<N, P, G, false, false>(a, i, base, h, st, factor);
+    if (vectors)
+      update<N, P, G, false, true>(a, i, base, h, st, factor);
+    else
+      update<N, P, G, false, false>(a, i, base, h, st, factor);
   }
 }
 
 template <int N>
-__global__ void __launch_bounds__(kThreads)
+__global__ void __launch_bounds__(kThreads, kBlocksPerSm)
     adamw_kernel(const __grid_constant__ Tensors<N> a, Hyper h, const float* factor_at, uint64_t seed, Workspace* ws) {
   const int lane = threadIdx.x & 31;
+  cudaGridDependencySynchronize();
   const float factor = factor_at ? *factor_at : 1.f;
   const int64_t tasks = a.first[a.n];
   int i = -1;
@@ -377,23 +392,36 @@ dg_status_t invalid(const char* msg) {
   return DG_ERR_INVALID_ARG;
 }
 
+bool aligned(const void* p, size_t to) { return (uintptr_t)p % to == 0; }
+
+// The list's tensors from `at` on, as many as fit; returns their tasks.
 template <int N>
-int64_t fill(const dg_adamw_tensor_t* t, int n, Tensors<N>* a) {
+int64_t fill(const dg_adamw_list_t& t, int64_t at, bool gradients_only, Tensors<N>* a) {
   int64_t tasks = 0;
-  for (int i = 0; i < n; ++i) {
-    a->param[i] = t[i].param;
-    a->grad[i] = t[i].grad;
-    a->m[i] = t[i].exp_avg;
-    a->v[i] = t[i].exp_avg_sq;
-    a->scales[i] = reinterpret_cast<float2*>(t[i].scales);
-    a->copy[i] = static_cast<__nv_bfloat16*>(t[i].copy);
-    a->step[i] = t[i].step;
-    a->count[i] = t[i].count;
-    a->id[i] = t[i].id;
-    a->flags[i] = (uint8_t)((t[i].param_type == DG_BF16 ? kParamBf16 : 0) | (t[i].grad_type == DG_BF16 ? kGradBf16 : 0) |
-                            (t[i].state_bits == 8 ? k8Bits : 0));
-    a->first[i] = tasks;
-    tasks += (t[i].count + kNumbers - 1) / kNumbers;
+  const int n = t.tensors - at < N ? (int)(t.tensors - at) : N;
+  for (int k = 0; k < n; ++k) {
+    const int64_t i = at + k;
+    int flags = t.grad_type[i] == DG_BF16 ? kGradBf16 : 0;
+    bool vectors = aligned(t.grad[i], t.grad_type[i] == DG_BF16 ? 8 : 16);
+    a->grad[k] = t.grad[i];
+    a->count[k] = t.numbers[i];
+    a->first[k] = tasks;
+    tasks += (t.numbers[i] + kNumbers - 1) / kNumbers;
+    if (!gradients_only) {
+      const bool bf16 = t.param_type[i] == DG_BF16, eight = t.state_bits[i] == 8;
+      a->param[k] = t.param[i];
+      a->m[k] = t.exp_avg[i];
+      a->v[k] = t.exp_avg_sq[i];
+      a->scales[k] = eight ? reinterpret_cast<float2*>(t.scales[i]) : nullptr;
+      a->copy[k] = t.copy ? static_cast<__nv_bfloat16*>(t.copy[i]) : nullptr;
+      a->step[k] = t.step[i];
+      a->id[k] = t.id ? t.id[i] : (uint32_t)i;
+      flags |= (bf16 ? kParamBf16 : 0) | (eight ? k8Bits : 0);
+      const size_t state = eight ? 4 : 16;
+      vectors = vectors && aligned(t.param[i], bf16 ? 8 : 16) && aligned(t.exp_avg[i], state) &&
+                aligned(t.exp_avg_sq[i], state) && aligned(a->copy[k], 8);
+    }
+    a->flags[k] = (uint8_t)(flags | (vectors ? kVectors : 0));
   }
   a->first[n] = tasks;
   a->n = n;
@@ -408,52 +436,57 @@ dg_status_t device_sms(int* sms) {
 }
 
 template <int N>
-dg_status_t step_launch(const dg_adamw_tensor_t* t, int n, const Hyper& h, const float* factor, uint64_t seed, Workspace* ws,
+dg_status_t step_launch(const dg_adamw_list_t& t, int64_t at, const Hyper& h, const float* factor, uint64_t seed, Workspace* ws,
                         int sms, cudaStream_t s) {
   Tensors<N> a;
-  const int64_t tasks = fill(t, n, &a);
+  const int64_t tasks = fill(t, at, false, &a);
   int64_t blocks = (tasks + kWarps - 1) / kWarps;
-  if (blocks > sms * 8) blocks = sms * 8;
+  if (blocks > sms * kBlocksPerSm) blocks = sms * kBlocksPerSm;
   if (blocks < 1) blocks = 1;  // tensors without numbers count their steps too
-  adamw_kernel<N><<<(unsigned)blocks, kThreads, 0, s>>>(a, h, factor, seed, ws);
-  DG_CUDA(cudaGetLastError());
+  DG_CUDA(launch_kernel(adamw_kernel<N>, dim3((unsigned)blocks), kThreads, s, true, a, h, factor, seed, ws));
   count_launches(1);
   return DG_OK;
 }
 
 template <int N>
-dg_status_t norm_launch(const dg_adamw_tensor_t* t, int n, bool first, bool last, float max_norm, Workspace* ws, float* result,
-                        cudaStream_t s) {
+dg_status_t norm_launch(const dg_adamw_list_t& t, int64_t at, float max_norm, Workspace* ws, float* result, cudaStream_t s) {
   Tensors<N> a;
-  fill(t, n, &a);
-  grad_norm_kernel<N><<<kNormBlocks, kThreads, 0, s>>>(a, first, last, max_norm, ws, result);
+  fill(t, at, true, &a);
+  grad_norm_kernel<N><<<kNormBlocks, kThreads, 0, s>>>(a, at == 0, at + a.n == t.tensors, max_norm, ws, result);
   DG_CUDA(cudaGetLastError());
   count_launches(1);
   return DG_OK;
 }
 
-dg_status_t check_list(int64_t count, const dg_adamw_tensor_t* t, const void* ws, bool gradients_only) {
-  if (count < 0 || count > ((int64_t)1 << 31)) return invalid("the number of tensors must be from 0 to 2^31");
-  if (count > 0 && !t) return invalid("tensors is NULL");
-  if (!ws || ((uintptr_t)ws & 255)) return invalid("workspace is NULL or not 256-byte aligned");
-  for (int64_t i = 0; i < count; ++i) {
-    const dg_adamw_tensor_t& e = t[i];
-    if (e.count < 0 || e.count > ((int64_t)1 << 40)) return invalid("a tensor's count must be from 0 to 2^40");
-    if (e.grad_type != DG_F32 && e.grad_type != DG_BF16) return invalid("a type must be DG_F32 or DG_BF16");
-    if (e.count > 0 && !e.grad) return invalid("a tensor's grad is NULL");
-    if ((uintptr_t)e.grad % (e.grad_type == DG_F32 ? 4 : 2)) return invalid("a gradient must be aligned to its type");
+dg_status_t check_list(const dg_adamw_list_t* list, const void* ws, bool gradients_only) {
+  if (!list) return invalid("list is NULL");
+  const dg_adamw_list_t& t = *list;
+  if (t.tensors < 0 || t.tensors > ((int64_t)1 << 31)) return invalid("the number of tensors must be from 0 to 2^31");
+  if (!ws || !aligned(ws, 256)) return invalid("workspace is NULL or not 256-byte aligned");
+  if (t.tensors == 0) return DG_OK;
+  if (!t.numbers || !t.grad || !t.grad_type) return invalid("an array of the list is NULL");
+  if (!gradients_only && (!t.param || !t.exp_avg || !t.exp_avg_sq || !t.step || !t.param_type || !t.state_bits))
+    return invalid("an array of the list is NULL");
+  for (int64_t i = 0; i < t.tensors; ++i) {
+    const bool some = t.numbers[i] > 0;
+    if (t.numbers[i] < 0 || t.numbers[i] > ((int64_t)1 << 40)) return invalid("a tensor must have from 0 to 2^40 numbers");
+    if (t.grad_type[i] != DG_F32 && t.grad_type[i] != DG_BF16) return invalid("a type must be DG_F32 or DG_BF16");
+    if (some && !t.grad[i]) return invalid("a tensor's grad is NULL");
+    if (!aligned(t.grad[i], t.grad_type[i] == DG_F32 ? 4 : 2)) return invalid("a gradient must be aligned to its type");
     if (gradients_only) continue;
-    if (e.param_type != DG_F32 && e.param_type != DG_BF16) return invalid("a type must be DG_F32 or DG_BF16");
-    if (e.state_bits != 8 && e.state_bits != 32) return invalid("state_bits must be 8 or 32");
-    if (!e.step || (uintptr_t)e.step % 8) return invalid("a tensor's step is NULL or misaligned");
-    if (e.copy && e.param_type != DG_F32) return invalid("a copy needs an fp32 param");
-    const uintptr_t state = e.state_bits == 32 ? 4 : 1;
-    if ((uintptr_t)e.param % (e.param_type == DG_F32 ? 4 : 2) || (uintptr_t)e.copy % 2 || (uintptr_t)e.exp_avg % state ||
-        (uintptr_t)e.exp_avg_sq % state)
+    if (t.param_type[i] != DG_F32 && t.param_type[i] != DG_BF16) return invalid("a type must be DG_F32 or DG_BF16");
+    if (t.state_bits[i] != 8 && t.state_bits[i] != 32) return invalid("state_bits must be 8 or 32");
+    if (!t.step[i] || !aligned(t.step[i], 8)) return invalid("a tensor's step is NULL or misaligned");
+    const void* copy = t.copy ? t.copy[i] : nullptr;
+    if (copy && t.param_type[i] != DG_F32) return invalid("a copy needs an fp32 param");
+    const size_t state = t.state_bits[i] == 32 ? 4 : 1;
+    if (!aligned(t.param[i], t.param_type[i] == DG_F32 ? 4 : 2) || !aligned(copy, 2) || !aligned(t.exp_avg[i], state) ||
+        !aligned(t.exp_avg_sq[i], state))
       return invalid("a tensor must be aligned to its type");
-    if (e.state_bits == 8 && (uintptr_t)e.scales % 8) return invalid("scales must be 8-byte aligned");
-    if (e.count > 0 && (!e.param || !e.exp_avg || !e.exp_avg_sq || (e.state_bits == 8 && !e.scales)))
-      return invalid("a tensor's pointer is NULL");
+    if (some && (!t.param[i] || !t.exp_avg[i] || !t.exp_avg_sq[i])) return invalid("a tensor's pointer is NULL");
+    if (t.state_bits[i] == 32) continue;
+    if (!t.scales || (some && !t.scales[i])) return invalid("8-bit states need scales");
+    if (!aligned(t.scales[i], 8)) return invalid("scales must be 8-byte aligned");
   }
   return DG_OK;
 }
@@ -463,39 +496,34 @@ dg_status_t check_list(int64_t count, const dg_adamw_tensor_t* t, const void* ws
 
 using namespace dg;
 
-extern "C" dg_status_t dg_grad_norm(int64_t count, const dg_adamw_tensor_t* tensors, float max_norm, void* workspace,
-                                    float* result, void* stream) {
-  if (dg_status_t st = check_list(count, tensors, workspace, true)) return st;
+extern "C" dg_status_t dg_grad_norm(const dg_adamw_list_t* list, float max_norm, void* workspace, float* result, void* stream) {
+  if (dg_status_t st = check_list(list, workspace, true)) return st;
   if (!(max_norm >= 0.f)) return invalid("max_norm must not be negative");
   if (!result) return invalid("result is NULL");
   Workspace* ws = static_cast<Workspace*>(workspace);
-  int64_t i = 0;
-  do {
-    const int n = count - i < kMost ? (int)(count - i) : kMost;
-    if (dg_status_t st = norm_launch<kMost>(tensors + i, n, i == 0, i + n == count, max_norm, ws, result, (cudaStream_t)stream))
-      return st;
-    i += n;
-  } while (i < count);
+  cudaStream_t s = (cudaStream_t)stream;
+  if (list->tensors <= kFew) return norm_launch<kFew>(*list, 0, max_norm, ws, result, s);
+  for (int64_t i = 0; i < list->tensors; i += kMost)
+    if (dg_status_t st = norm_launch<kMost>(*list, i, max_norm, ws, result, s)) return st;
   return DG_OK;
 }
 
-extern "C" dg_status_t dg_adamw_step(int64_t count, const dg_adamw_tensor_t* tensors, double lr, double beta1, double beta2,
-                                     double eps, double weight_decay, const float* grad_factor, uint64_t seed, void* workspace,
+extern "C" dg_status_t dg_adamw_step(const dg_adamw_list_t* list, double lr, double beta1, double beta2, double eps,
+                                     double weight_decay, const float* grad_factor, uint64_t seed, void* workspace,
                                      void* stream) {
-  if (dg_status_t st = check_list(count, tensors, workspace, false)) return st;
+  if (dg_status_t st = check_list(list, workspace, false)) return st;
   if (!(beta1 >= 0.0 && beta1 < 1.0 && beta2 >= 0.0 && beta2 < 1.0)) return invalid("beta1 and beta2 must be in [0, 1)");
   if (!(lr >= 0.0 && lr < INFINITY) || !(eps >= 0.0 && eps < INFINITY) || !(weight_decay >= 0.0 && weight_decay < INFINITY))
     return invalid("lr, eps and weight_decay must be finite and not negative");
-  if (count == 0) return DG_OK;
-  Hyper h{lr, log2(beta1), log2(beta2), (float)(1.0 - beta1), (float)beta2, (float)(1.0 - beta2), (float)eps,
-          (float)(1.0 - lr * weight_decay)};
+  if (list->tensors == 0) return DG_OK;
+  const Hyper h{lr, log2(beta1), log2(beta2), (float)(1.0 - beta1), (float)beta2, (float)(1.0 - beta2), (float)eps,
+                (float)(1.0 - lr * weight_decay)};
   int sms = 0;
   if (dg_status_t st = device_sms(&sms)) return st;
-  for (int64_t i = 0; i < count; i += kMost) {
-    const int n = count - i < kMost ? (int)(count - i) : kMost;
-    if (dg_status_t st = step_launch<kMost>(tensors + i, n, h, grad_factor, seed, static_cast<Workspace*>(workspace), sms,
-                                            (cudaStream_t)stream))
-      return st;
-  }
+  Workspace* ws = static_cast<Workspace*>(workspace);
+  cudaStream_t s = (cudaStream_t)stream;
+  if (list->tensors <= kFew) return step_launch<kFew>(*list, 0, h, grad_factor, seed, ws, sms, s);
+  for (int64_t i = 0; i < list->tensors; i += kMost)
+    if (dg_status_t st = step_launch<kMost>(*list, i, h, grad_factor, seed, ws, sms, s)) return st;
   return DG_OK;
 }

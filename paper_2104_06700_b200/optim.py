@@ -82,29 +82,23 @@ class AdamW(torch.optim.Optimizer):
             state["master"] = p.detach().float()
         return state
 
-    def _tensors(self, group, first: int) -> list:
-        """The group's tensors for the library; the random bits of the i-th go by first + i."""
-        tensors = []
+    def _take(self, group, first: int, lists) -> None:
+        """Adds the group's tensors to the lists; the random bits of the i-th go by first + i."""
         for i, p in enumerate(group["params"], first):
             g = p.grad
             if g is None:
                 continue
             if g.is_sparse:
                 raise ValueError("sparse gradients are not supported")
-            if self._device is None:
-                self._device = p.device
-            elif p.device != self._device:
-                raise ValueError(f"parameters are on {self._device} and on {p.device}: one step runs on one device")
             s = self.state[p]
             if not s:
                 s.update(self._new_state(p, group))
-            if not g.is_contiguous():
-                g = g.contiguous()
-                self._kept.append(g)        # until the launch is queued; the allocator's stream order does the rest
             master = s.get("master")
-            target, copy = (p, None) if master is None else (master, p)
-            tensors.append(binding.adamw_tensor(target, g, s["exp_avg"], s["exp_avg_sq"], s["step"], s.get("scales"), copy, i))
-        return tensors
+            # a gradient in another order: the copy lives until the launch, then the allocator's stream order serves
+            row = (g if g.is_contiguous() else g.contiguous(), p if master is None else master, s["exp_avg"], s["exp_avg_sq"],
+                   s["step"], s.get("scales"), None if master is None else p, i)
+            for column, value in zip(lists, row):
+                column.append(value)
 
     @torch.no_grad()
     def step(self, closure=None):
@@ -112,22 +106,24 @@ class AdamW(torch.optim.Optimizer):
         if closure is not None:
             with torch.enable_grad():
                 loss = closure()
-        self._kept, self._device, lists, first = [], None, [], 0
+        parts, first = [], 0
         for group in self.param_groups:
-            lists.append(self._tensors(group, first))
+            lists = [[] for _ in range(8)]
+            self._take(group, first, lists)
             first += len(group["params"])
-        every = [t for tensors in lists for t in tensors]
-        if every:
-            if self._device.index == torch.cuda.current_device():
-                self._launch(lists, every)
+            if lists[0]:
+                parts.append((group, lists))
+        if parts:
+            device = parts[0][1][0][0].device
+            if device.index == torch.cuda.current_device():
+                self._launch(parts, device)
             else:
-                with torch.cuda.device(self._device):
-                    self._launch(lists, every)
-        self._kept = []
+                with torch.cuda.device(device):
+                    self._launch(parts, device)
         return loss
 
-    def _launch(self, lists, every) -> None:
-        device = self._device
+    def _launch(self, parts, device) -> None:
+        tables = [binding.AdamwList(*lists) for _, lists in parts]
         if self._workspace is None or self._workspace.device != device:
             if torch.cuda.is_current_stream_capturing():
                 raise RuntimeError("run a step before capturing one")
@@ -135,10 +131,10 @@ class AdamW(torch.optim.Optimizer):
             self._result = torch.zeros(2, dtype=torch.float32, device=device)
         factor = None
         if self.max_norm is not None:
+            every = tables[0] if len(tables) == 1 else binding.AdamwList([g for _, lists in parts for g in lists[0]])
             binding.dg_grad_norm(every, self.max_norm, self._workspace, self._result)
             self.grad_norm, factor = self._result[0], self._result[1]
-        for group, tensors in zip(self.param_groups, lists):
-            if tensors:
-                beta1, beta2 = group["betas"]
-                binding.dg_adamw_step(tensors, group["lr"], beta1, beta2, group["eps"], group["weight_decay"], self._workspace,
-                                      factor, group["seed"])
+        for (group, _), table in zip(parts, tables):
+            beta1, beta2 = group["betas"]
+            binding.dg_adamw_step(table, group["lr"], beta1, beta2, group["eps"], group["weight_decay"], self._workspace,
+                                  factor, group["seed"])

@@ -1,6 +1,7 @@
 """What dg_adamw_step, dg_grad_norm and optim.AdamW refuse, and their host side, without a GPU."""
 import ctypes
 import struct
+from array import array
 
 import pytest
 import torch
@@ -10,32 +11,46 @@ from test_host_side import fake, library  # noqa: F401
 
 i64, f32, f64 = ctypes.c_int64, ctypes.c_float, ctypes.c_double
 OK, BAD = binding.DG_OK, binding.DG_ERR_INVALID_ARG
-NAMES = ("param", "grad", "exp_avg", "exp_avg_sq", "scales", "copy", "step", "count", "param_type", "grad_type", "state_bits", "id")
+FIELDS = dict(numbers="q", param="Q", grad="Q", exp_avg="Q", exp_avg_sq="Q", scales="Q", copy="Q", step="Q", param_type="i",
+              grad_type="i", state_bits="i", id="I")       # dg_adamw_list_t, behind `tensors`
 
 
 def tensor(fake, n=300, **changed):
     a = lambda count: (fake.array(count + 4).value + 15) // 16 * 16  # noqa: E731
-    t = dict(zip(NAMES, (a(n), a(n), a(n), a(n), 0, 0, a(2), n, 0, 0, 32, 0)))
-    t.update(changed)
-    return binding._adamw_tensor(*t.values())
+    return {**dict(zip(FIELDS, (n, a(n), a(n), a(n), a(n), 0, 0, a(2), 0, 0, 32, 0))), **changed}
+
+
+def listed(fake, tensors, count=None, absent=()):
+    """A dg_adamw_list_t; arrays named in `absent` are NULL."""
+    columns = {k: array(code, [t[k] for t in tensors]) for k, code in FIELDS.items()}
+    fake.keep.append(columns)
+    where = [0 if k in absent else c.buffer_info()[0] for k, c in columns.items()]
+    return struct.pack("q12Q", len(tensors) if count is None else count, *where)
 
 
 def workspace(fake, shift=0):
     return ctypes.c_void_p((fake.array(4096).value + 255) // 256 * 256 + shift)
 
 
-def step(fake, *tensors, ws=None, lr=1e-3, beta1=0.9, beta2=0.999, eps=1e-8, decay=0.0, count=None):
-    return fake.lib.dg_adamw_step(i64(len(tensors) if count is None else count), b"".join(tensors) or None, f64(lr), f64(beta1),
-                                  f64(beta2), f64(eps), f64(decay), None, ctypes.c_uint64(1), ws or workspace(fake), None)
+def step(fake, *tensors, ws=None, lr=1e-3, beta1=0.9, beta2=0.999, eps=1e-8, decay=0.0, count=None, absent=()):
+    return fake.lib.dg_adamw_step(listed(fake, tensors, count, absent), f64(lr), f64(beta1), f64(beta2), f64(eps), f64(decay),
+                                  None, ctypes.c_uint64(1), ws or workspace(fake), None)
 
 
-def norm(fake, *tensors, ws=None, max_norm=1.0, result=True):
-    return fake.lib.dg_grad_norm(i64(len(tensors)), b"".join(tensors) or None, f32(max_norm), ws or workspace(fake),
+def norm(fake, *tensors, ws=None, max_norm=1.0, result=True, absent=()):
+    return fake.lib.dg_grad_norm(listed(fake, tensors, None, absent), f32(max_norm), ws or workspace(fake),
                                  fake.array(2) if result else None, None)
 
 
-def test_the_struct_is_the_headers():
-    assert struct.calcsize("7Qq3iI") == 80
+def test_lists_with_arrays_left_out(fake):
+    t = tensor(fake)
+    assert step(fake, t, absent=("scales", "copy", "id")) == OK
+    assert step(fake, tensor(fake, state_bits=8), absent=("scales",)) == BAD
+    for name in set(FIELDS) - {"scales", "copy", "id"}:
+        assert step(fake, t, absent=(name,)) == BAD, name
+        assert norm(fake, t, absent=(name,)) == (BAD if name in ("numbers", "grad", "grad_type") else OK), name
+    assert fake.lib.dg_adamw_step(None, f64(0), f64(0), f64(0), f64(0), f64(0), None, ctypes.c_uint64(1), workspace(fake), None) == BAD
+    assert fake.lib.dg_grad_norm(None, f32(1), workspace(fake), fake.array(2), None) == BAD
 
 
 def test_lists_that_are_refused(fake):
@@ -47,10 +62,10 @@ def test_lists_that_are_refused(fake):
                   dict(exp_avg_sq=4098), dict(copy=4097), dict(step=4100), dict(state_bits=8, scales=4100)):
         assert step(fake, tensor(fake), tensor(fake, **wrong)) == BAD, wrong
         assert norm(fake, tensor(fake), tensor(fake, **wrong)) == OK, wrong
-    for wrong in (dict(grad=0), dict(count=-1), dict(count=(1 << 40) + 1), dict(grad_type=2), dict(grad=4098),
+    for wrong in (dict(grad=0), dict(numbers=-1), dict(numbers=(1 << 40) + 1), dict(grad_type=2), dict(grad=4098),
                   dict(grad_type=1, grad=4097)):
         assert step(fake, tensor(fake, **wrong)) == BAD and norm(fake, tensor(fake, **wrong)) == BAD, wrong
-    assert step(fake, count=1) == BAD and step(fake, count=-1) == BAD
+    assert step(fake, count=-1) == BAD and step(fake, tensor(fake), count=(1 << 31) + 1) == BAD
     for shift in (8, 128):
         assert step(fake, tensor(fake), ws=workspace(fake, shift)) == BAD
         assert norm(fake, tensor(fake), ws=workspace(fake, shift)) == BAD
@@ -90,6 +105,4 @@ def test_the_optimiser_checks_its_options():
     with pytest.raises(ValueError, match="CUDA"):
         opt.step()
     with pytest.raises(ValueError, match="CUDA"):
-        binding.adamw_tensor(p, p, p, p, p)
-    with pytest.raises(ValueError, match="CUDA"):
-        binding.gradient_tensor(p)
+        binding.AdamwList([p])

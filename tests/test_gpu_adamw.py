@@ -43,10 +43,6 @@ class Tensor:
             self.scales, self.m, self.v = None, place(m), place(u * u)
         self.step = torch.tensor(taken, device=DEV)
 
-    def given(self):
-        return binding.adamw_tensor(self.p if self.master is None else self.master, self.grad, self.m, self.v, self.step,
-                                    self.scales, None if self.master is None else self.p, self.id)
-
     def snapshot(self):
         if self.bits == 8:
             m, v = ref.decoded(self.m, self.scales, 0), ref.decoded(self.v, self.scales, 1).square()
@@ -89,8 +85,15 @@ class Tensor:
             ref.close(self.v, v, d_v + 2.0 ** -149)
 
 
+def given(tensors):
+    masters = [t.p if t.master is None else t.master for t in tensors]
+    return binding.AdamwList([t.grad for t in tensors], masters, [t.m for t in tensors], [t.v for t in tensors],
+                             [t.step for t in tensors], [t.scales for t in tensors],
+                             [None if t.master is None else t.p for t in tensors], [t.id for t in tensors])
+
+
 def step(tensors, **more):
-    binding.dg_adamw_step([t.given() for t in tensors], workspace=binding.adamw_workspace(DEV), **{**HYPER, **more})
+    binding.dg_adamw_step(given(tensors), workspace=binding.adamw_workspace(DEV), **{**HYPER, **more})
 
 
 KINDS = [(F32, F32, False), (BF16, BF16, False), (F32, BF16, False), (BF16, F32, False), (BF16, BF16, True), (BF16, F32, True)]
@@ -118,19 +121,19 @@ def test_any_alignment_and_mixed_lists(bits, shift):
         t.check(b)
 
 
-@pytest.mark.parametrize("count", [400, 401, 1234])
+@pytest.mark.parametrize("count", [24, 25, 400, 401, 1234])
 def test_lists_longer_than_a_launch(count):
     tensors = [Tensor(1 + (37 * i) % 600, F32, F32, (32, 8)[i % 2], i, taken=i % 5) for i in range(count)]
     before = [t.snapshot() for t in tensors]
     norm = torch.zeros(2, device=DEV)
     workspace = binding.adamw_workspace(DEV)
     total = sum(t.grad.double().square().sum() for t in tensors).sqrt()
-    given = [t.given() for t in tensors]
+    listed = given(tensors)
     for _ in range(2):
-        binding.dg_grad_norm(given, 0.5, workspace, norm)
+        binding.dg_grad_norm(listed, 0.5, workspace, norm)
         ref.close(norm[:1], total, 2 * U * total)
         ref.close(norm[1:], 0.5 / (total + 1e-6), 4 * U * norm[1].double())
-    binding.dg_adamw_step(given, workspace=workspace, grad_factor=norm[1:], **HYPER)
+    binding.dg_adamw_step(listed, workspace=workspace, grad_factor=norm[1:], **HYPER)
     for t, b in zip(tensors, before):
         t.check(b, factor=float(0.5 / (total + 1e-6)), factor_off=8 * U)
     assert not bool(workspace[:8].any())       # the tickets are back at 0
@@ -143,17 +146,17 @@ def test_norm_of_gradients(sizes, types):
     for scale in (1.0, 1e-30, 1e25):
         grads = [(torch.randn(n, device=DEV, generator=gen) * scale).to(types) for n in sizes]
         want = torch.cat([g.double() for g in grads]).norm()
-        tensors = [binding.gradient_tensor(g) for g in grads]
+        tensors = binding.AdamwList(grads)
         binding.dg_grad_norm(tensors, 1.0, workspace, result)
         first = result.clone()
         ref.close(result[:1], want, 2 * U * want)
         ref.close(result[1:], (1 / (want + 1e-6)).clamp(max=1.0), 4 * U * (1 / (want + 1e-6)).clamp(max=1.0))
         binding.dg_grad_norm(tensors, 1.0, workspace, result)
         assert torch.equal(first, result)
-    binding.dg_grad_norm([], 1.0, workspace, result)
+    binding.dg_grad_norm(binding.AdamwList([]), 1.0, workspace, result)
     assert result.tolist() == [0.0, 1.0]
     bad = torch.tensor([1.0, float("nan")], device=DEV)
-    binding.dg_grad_norm([binding.gradient_tensor(bad)], 1.0, workspace, result)
+    binding.dg_grad_norm(binding.AdamwList([bad]), 1.0, workspace, result)
     assert result.isnan().all()
 
 
@@ -227,7 +230,7 @@ def test_more_numbers_than_32_bits_count(n):
     scales = torch.zeros((n + 255) // 256, 2, device=DEV)
     count = torch.zeros((), dtype=torch.int64, device=DEV)
     result = torch.zeros(2, device=DEV)
-    tensors = [binding.adamw_tensor(p, grad, m, v, count, scales, None, 9)]
+    tensors = binding.AdamwList([grad], [p], [m], [v], [count], [scales], ids=[9])
     workspace = binding.adamw_workspace(DEV)
     binding.dg_grad_norm(tensors, 1e9, workspace, result)
     assert float(result[0]) == pytest.approx(0.25 * n ** 0.5, rel=1e-6)
