@@ -17,6 +17,8 @@ constexpr int kThreads = 256;
 constexpr int kWarps = kThreads / 32;
 constexpr int kBlocksPerSm = 3;                     // what 80 registers a thread leave room for
 constexpr int kNumbers = 256;                       // of a warp's task: 8 a lane, and one scale
+constexpr int kBlocksPerTask = 4;
+constexpr int kNormNumbers = 2048;                  // of a warp's task of the norm
 constexpr int kNormBlocks = 148 * 4;
 constexpr float kLargest = 448.f;                   // of e4m3
 constexpr float kLeastScale = 0x1p-126f;            // its inverse is finite
@@ -35,6 +37,7 @@ struct Tensors {
   int64_t* step[N];
   int64_t count[N];
   int64_t first[N + 1];  // tasks before tensor i's
+  int32_t numbers;       // of a task: a multiple of 256
   uint32_t id[N];
   uint8_t flags[N];
   int32_t n;
@@ -49,7 +52,8 @@ static_assert(sizeof(Workspace) <= DG_ADAMW_WORKSPACE_BYTES, "dg.h promises less
 
 struct Hyper {
   double lr, log2_beta1, log2_beta2;
-  float rest1, beta2, rest2, eps, decay;  // 1 - beta1, beta2, 1 - beta2, eps, 1 - lr wd
+  float beta1, rest1, beta2, rest2, eps, decay;  // beta1, 1 - beta1, beta2, 1 - beta2, eps, 1 - lr wd
+  float root2, root_rest2;                       // sqrt(beta2), sqrt(1 - beta2)
 };
 
 // A 32-bit hash: lowbias32 of Chris Wellons.
@@ -131,26 +135,49 @@ __device__ __forceinline__ void store_bytes(uint8_t* p, int left, uint32_t v) {
   }
 }
 
-// The number an e4m3 code stands for: exponents from -6 on, steps of 2^-9 below 2^-6; 0x7f is NaN.
-__device__ __forceinline__ float from_e4m3(uint32_t code) {
-  const uint32_t rest = code & 0x7f;
-  // the seven bits in fp32's place stand for the number times 2^-120
-  float v = __uint_as_float(rest << 20) * 0x1p120f;
-  if (rest == 0x7f) v = NAN;
-  return code & 0x80 ? -v : v;
+// Two numbers side by side: one instruction for both.
+struct Two {
+  uint64_t v;
+};
+__device__ __forceinline__ Two two(float a, float b) {
+  Two r;
+  asm("mov.b64 %0, {%1, %2};" : "=l"(r.v) : "f"(a), "f"(b));
+  return r;
+}
+__device__ __forceinline__ Two both(float a) { return two(a, a); }
+__device__ __forceinline__ float2 apart(Two a) {
+  float2 r;
+  asm("mov.b64 {%0, %1}, %2;" : "=f"(r.x), "=f"(r.y) : "l"(a.v));
+  return r;
+}
+__device__ __forceinline__ Two operator*(Two a, Two b) {
+  Two r;
+  asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r.v) : "l"(a.v), "l"(b.v));
+  return r;
+}
+__device__ __forceinline__ Two fma2(Two a, Two b, Two c) {
+  Two r;
+  asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r.v) : "l"(a.v), "l"(b.v), "l"(c.v));
+  return r;
+}
+
+// What two e4m3 codes stand for.
+__device__ __forceinline__ Two from_e4m3(uint32_t codes) {
+  float a, b;
+  asm("{ .reg .b16 c, lo, hi; .reg .b32 h; cvt.u16.u32 c, %2; cvt.rn.f16x2.e4m3x2 h, c; mov.b32 {lo, hi}, h;"
+      " cvt.f32.f16 %0, lo; cvt.f32.f16 %1, hi; }"
+      : "=f"(a), "=f"(b)
+      : "r"(codes));
+  return two(a, b);
 }
 
 // An 8-bit state is rounded up with a probability that is its distance from the lower neighbour: the averages move by a
 // thousandth of themselves a step, far less than half a step of 3 bits, and rounding to nearest would hold them where they
-// are.  y >= 0 or NaN; r: 16 random bits.  In [2^-6, 448] the three mantissa bits to keep are followed by 20: adding the
-// random ones there carries into them.  2^-6 more gives the smaller numbers, evenly 2^-9 apart, the same form.
-__device__ __forceinline__ uint32_t to_e4m3(float y, uint32_t r) {
-  if (y != y || y == INFINITY) return 0x7f;
-  y = fminf(y, kLargest);
-  const bool small = y < 0x1p-6f;
-  if (small) y += 0x1p-6f;
-  const uint32_t code = ((__float_as_uint(y) + (r << 4) + 8u) >> 20) - (small ? 968u : 960u);
-  return code < 126u ? code : 126u;
+// are.  `in_front`: the number times 2^-120, at most 448 of them up to a rounding: it has e4m3's bits in front, denormal
+// ones too, and 20 behind them; adding 16 random bits `r` there carries into them.
+__device__ __forceinline__ uint32_t to_e4m3(float in_front, uint32_t r) {
+  const uint32_t code = (__float_as_uint(in_front) + (r << 4) + 8u) >> 20;
+  return min(code, 126u);
 }
 
 // A bf16 parameter is rounded up or down by 16 random bits too: steps of a thousandth of it would all be lost to nearest.
@@ -160,24 +187,58 @@ __device__ __forceinline__ uint32_t to_bf16_random(float p, uint32_t r) {
   return (bits + (r & 0xffffu)) >> 16;
 }
 
-__device__ __forceinline__ float warp_max(float v) {
-#pragma unroll
-  for (int o = 16; o > 0; o >>= 1) v = fmaxf(v, __shfl_xor_sync(0xffffffffu, v, o));
-  return v;
-}
-// off by at most 2^-23 of itself
+// off by at most 2^-23 of itself; numbers below 2^-126 count as 0
 __device__ __forceinline__ float fast_sqrt(float v) {
   float r;
-  asm("sqrt.approx.f32 %0, %1;" : "=f"(r) : "f"(v));
+  asm("sqrt.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(v));
   return r;
 }
-// the largest of the finite ones: a number that is not finite keeps to itself
-__device__ __forceinline__ float finite_max(float m, float v) { return v < INFINITY ? fmaxf(m, v) : m; }
+// 1 / v, off by at most 2^-23 of itself
+__device__ __forceinline__ float fast_inverse(float v) {
+  float r;
+  asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(v));
+  return r;
+}
+// The larger magnitude, NaN if one is.
+__device__ __forceinline__ float most_of(float a, float b) {
+  float r;
+  asm("max.NaN.f32 %0, %1, %2;" : "=f"(r) : "f"(a), "f"(fabsf(b)));
+  return r;
+}
+__device__ __forceinline__ float warp_most(float v) {
+  float r;
+  asm("redux.sync.max.NaN.f32 %0, %1, 0xffffffff;" : "=f"(r) : "f"(v));
+  return r;
+}
+// The largest of a warp's finite ones: a number that is not finite keeps to itself.
+__device__ float warp_most_finite(const float (&v)[8]) {
+  float m = 0.f;
+#pragma unroll
+  for (int j = 0; j < 8; ++j) m = fabsf(v[j]) < INFINITY ? fmaxf(m, fabsf(v[j])) : m;
+  return warp_most(m);
+}
 
 struct Step {
   float c1, c2;   // lr / (1 - b1^t), 1 / sqrt(1 - b2^t)
   uint32_t key;
 };
+
+template <typename P, bool VEC, int N>
+__device__ __forceinline__ void store_param(const Tensors<N>& a, int i, int64_t q, int left, const float* p, const uint32_t* r) {
+  uint32_t c[4];
+  if constexpr (sizeof(P) == 4) {
+    store4<VEC>(static_cast<float*>(a.param[i]) + q, left, p);
+    if (a.copy[i]) {  // the master weights keep what the copy loses: to nearest
+#pragma unroll
+      for (int j = 0; j < 4; ++j) c[j] = __bfloat16_as_ushort(__float2bfloat16_rn(p[j]));
+      store4<VEC>(reinterpret_cast<uint16_t*>(a.copy[i]) + q, left, c);
+    }
+  } else {
+#pragma unroll
+    for (int j = 0; j < 4; ++j) c[j] = to_bf16_random(p[j], r[j]);
+    store4<VEC>(static_cast<uint16_t*>(a.param[i]) + q, left, c);
+  }
+}
 
 // One task: the numbers base .. base + 255 of a tensor, as far as it goes.  A lane has four at 4 lane, four 128 further.
 template <int N, typename P, typename G, bool EIGHT, bool VEC>
@@ -185,7 +246,8 @@ __device__ __forceinline__ void update(const Tensors<N>& a, int i, int64_t base,
   const int lane = threadIdx.x & 31;
   const int64_t at = base + 4 * lane, end = a.count[i];
   const uint32_t key = mix(st.key ^ (uint32_t)(base >> 32));
-  float p[8], g[8], m[8], v[8];
+  float p[8], g[8], m[8], v[8];   // EIGHT: v is sqrt(v)
+  Two m2[4], u2[4];
   float2 scale = make_float2(0.f, 0.f);
   if (EIGHT) scale = a.scales[i][base / kNumbers];
 #pragma unroll
@@ -197,97 +259,112 @@ __device__ __forceinline__ void update(const Tensors<N>& a, int i, int64_t base,
     if constexpr (EIGHT) {
       const uint32_t mb = load_bytes<VEC>(static_cast<const uint8_t*>(a.m[i]) + q, left);
       const uint32_t ub = load_bytes<VEC>(static_cast<const uint8_t*>(a.v[i]) + q, left);
-#pragma unroll
-      for (int j = 0; j < 4; ++j) {
-        m[4 * k + j] = from_e4m3(mb >> (8 * j) & 0xff) * scale.x;
-        const float u = from_e4m3(ub >> (8 * j) & 0xff) * scale.y;
-        v[4 * k + j] = u * u;
-      }
+      m2[2 * k] = from_e4m3(mb), m2[2 * k + 1] = from_e4m3(mb >> 16);
+      u2[2 * k] = from_e4m3(ub), u2[2 * k + 1] = from_e4m3(ub >> 16);
     } else {
       load4<float, VEC>(static_cast<const float*>(a.m[i]) + q, left, m + 4 * k);
       load4<float, VEC>(static_cast<const float*>(a.v[i]) + q, left, v + 4 * k);
     }
   }
-  float most_m = 0.f, most_u = 0.f;
-  float u[8];
+  if constexpr (EIGHT) {
+    // scales and betas in one factor of each code
+    const Two keep_m = both(h.beta1 * scale.x), keep_u = both(h.root2 * scale.y);
+    const Two take_m = both(h.rest1 * factor), take_u = both(h.root_rest2 * factor);
+    float most_m = 0.f, most_u = 0.f;
 #pragma unroll
-  for (int j = 0; j < 8; ++j) {
-    const float gj = g[j] * factor;
-    m[j] = fmaf(h.rest1, gj - m[j], m[j]);
-    v[j] = fmaf(h.rest2 * gj, gj, h.beta2 * v[j]);
-    u[j] = fast_sqrt(v[j]);
-    p[j] = fmaf(p[j], h.decay, -st.c1 * __fdividef(m[j], fmaf(u[j], st.c2, h.eps)));
-    if (EIGHT) {
-      most_m = finite_max(most_m, fabsf(m[j]));
-      most_u = finite_max(most_u, u[j]);
+    for (int j = 0; j < 4; ++j) {
+      const Two gj = two(g[2 * j], g[2 * j + 1]), old = u2[j] * keep_u, now = gj * take_u;
+      m2[j] = fma2(m2[j], keep_m, gj * take_m);
+      const float2 vj = apart(fma2(old, old, now * now)), mj = apart(m2[j]);
+      v[2 * j] = fast_sqrt(vj.x), v[2 * j + 1] = fast_sqrt(vj.y);
+      const float2 under = apart(fma2(two(v[2 * j], v[2 * j + 1]), both(st.c2), both(h.eps)));
+      const Two ratio = m2[j] * two(fast_inverse(under.x), fast_inverse(under.y));
+      const float2 pj = apart(fma2(ratio, both(-st.c1), two(p[2 * j], p[2 * j + 1]) * both(h.decay)));
+      p[2 * j] = pj.x, p[2 * j + 1] = pj.y;
+      m[2 * j] = mj.x, m[2 * j + 1] = mj.y;
+      most_m = most_of(most_of(most_m, mj.x), mj.y);
+      most_u = most_of(most_of(most_u, v[2 * j]), v[2 * j + 1]);
     }
-  }
-  float inv_m = 0.f, inv_u = 0.f;
-  if (EIGHT) {
-    const float sm = fmaxf(__fdiv_rn(warp_max(most_m), kLargest), kLeastScale);
-    const float su = fmaxf(__fdiv_rn(warp_max(most_u), kLargest), kLeastScale);
-    inv_m = __frcp_rn(sm);
-    inv_u = __frcp_rn(su);
-    if (lane == 0) a.scales[i][base / kNumbers] = make_float2(sm, su);
-  }
-#pragma unroll
-  for (int k = 0; k < 2; ++k) {
-    const int64_t q = at + 128 * k;
-    const int left = VEC ? 4 : (int)(end - q < 0 ? 0 : end - q < 4 ? end - q : 4);
-    uint32_t r[4] = {};
-    if (EIGHT || sizeof(P) == 2) {
-#pragma unroll
-      for (int j = 0; j < 4; ++j) r[j] = mix((uint32_t)(q + j) + key);
+    most_m = warp_most(most_m);
+    most_u = warp_most(most_u);
+    const bool careful = !(most_m < INFINITY && most_u < INFINITY);  // of the whole warp
+    if (careful) {
+      most_m = warp_most_finite(m);
+      most_u = warp_most_finite(v);
     }
-    if constexpr (sizeof(P) == 4) {
-      store4<VEC>(static_cast<float*>(a.param[i]) + q, left, p + 4 * k);
-      if (a.copy[i]) {  // the master weights keep what the copy loses: to nearest
-        uint32_t c[4];
+    scale.x = fmaxf(__fdiv_rn(most_m, kLargest), kLeastScale);
+    scale.y = fmaxf(__fdiv_rn(most_u, kLargest), kLeastScale);
+    if (lane == 0) a.scales[i][base / kNumbers] = scale;
+    const Two inv_m = both(__frcp_rn(scale.x)), inv_u = both(__frcp_rn(scale.y)), front = both(0x1p-120f);
+    float ym[8], yu[8];
 #pragma unroll
-        for (int j = 0; j < 4; ++j) c[j] = __bfloat16_as_ushort(__float2bfloat16_rn(p[4 * k + j]));
-        store4<VEC>(reinterpret_cast<uint16_t*>(a.copy[i]) + q, left, c);
-      }
-    } else {
-      uint32_t c[4];
-#pragma unroll
-      for (int j = 0; j < 4; ++j) c[j] = to_bf16_random(p[4 * k + j], r[j]);
-      store4<VEC>(static_cast<uint16_t*>(a.param[i]) + q, left, c);
+    for (int j = 0; j < 4; ++j) {
+      const float2 a2 = apart(two(m[2 * j], m[2 * j + 1]) * inv_m * front), b2 = apart(two(v[2 * j], v[2 * j + 1]) * inv_u * front);
+      ym[2 * j] = a2.x, ym[2 * j + 1] = a2.y;
+      yu[2 * j] = b2.x, yu[2 * j + 1] = b2.y;
     }
-    if constexpr (EIGHT) {
-      uint32_t mb = 0, ub = 0;
+#pragma unroll
+    for (int k = 0; k < 2; ++k) {
+      const int64_t q = at + 128 * k;
+      const int left = VEC ? 4 : (int)(end - q < 0 ? 0 : end - q < 4 ? end - q : 4);
+      uint32_t r[4], cm[4], cu[4];
 #pragma unroll
       for (int j = 0; j < 4; ++j) {
-        const float mj = m[4 * k + j], uj = u[4 * k + j];
-        const uint32_t cm = to_e4m3(fabsf(mj) * inv_m, r[j] & 0xffff) | (mj < 0.f ? 0x80u : 0u);
-        uint32_t cu = to_e4m3(uj * inv_u, r[j] >> 16);
-        if (uj > 0.f && cu == 0) cu = 1;  // a denominator that was not 0 does not become 0
-        mb |= cm << (8 * j);
-        ub |= cu << (8 * j);
+        const float mj = m[4 * k + j], uj = v[4 * k + j];
+        r[j] = mix((uint32_t)(q + j) + key);
+        cm[j] = to_e4m3(fabsf(ym[4 * k + j]), r[j] & 0xffff);
+        cu[j] = to_e4m3(yu[4 * k + j], r[j] >> 16);
+        cu[j] = max(cu[j], min(__float_as_uint(uj), 1u));  // a denominator that was not 0 does not become 0
+        if (careful) {
+          if (!(fabsf(mj) < INFINITY)) cm[j] = 0x7f;
+          if (!(uj < INFINITY)) cu[j] = 0x7f;
+        }
+        cm[j] |= __float_as_uint(mj) >> 24 & 0x80u;
       }
-      store_bytes<VEC>(static_cast<uint8_t*>(a.m[i]) + q, left, mb);
-      store_bytes<VEC>(static_cast<uint8_t*>(a.v[i]) + q, left, ub);
-    } else {
+      store_param<P, VEC>(a, i, q, left, p + 4 * k, r);
+      store_bytes<VEC>(static_cast<uint8_t*>(a.m[i]) + q, left, __byte_perm(__byte_perm(cm[0], cm[1], 0x0040), __byte_perm(cm[2], cm[3], 0x0040), 0x5410));
+      store_bytes<VEC>(static_cast<uint8_t*>(a.v[i]) + q, left, __byte_perm(__byte_perm(cu[0], cu[1], 0x0040), __byte_perm(cu[2], cu[3], 0x0040), 0x5410));
+    }
+  } else {
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+      const float gj = g[j] * factor;
+      m[j] = fmaf(h.rest1, gj - m[j], m[j]);
+      v[j] = fmaf(h.rest2 * gj, gj, h.beta2 * v[j]);
+      p[j] = fmaf(p[j], h.decay, -st.c1 * (m[j] * fast_inverse(fmaf(sqrtf(v[j]), st.c2, h.eps))));
+    }
+#pragma unroll
+    for (int k = 0; k < 2; ++k) {
+      const int64_t q = at + 128 * k;
+      const int left = VEC ? 4 : (int)(end - q < 0 ? 0 : end - q < 4 ? end - q : 4);
+      uint32_t r[4] = {};
+      if (sizeof(P) == 2) {
+#pragma unroll
+        for (int j = 0; j < 4; ++j) r[j] = mix((uint32_t)(q + j) + key);
+      }
+      store_param<P, VEC>(a, i, q, left, p + 4 * k, r);
       store4<VEC>(static_cast<float*>(a.m[i]) + q, left, m + 4 * k);
       store4<VEC>(static_cast<float*>(a.v[i]) + q, left, v + 4 * k);
     }
   }
 }
 
+template <int N, typename P, typename G, bool EIGHT>
+__device__ __forceinline__ void update_run(const Tensors<N>& a, int i, int64_t base, int64_t end, const Hyper& h, const Step& st,
+                                           float factor) {
+  if (a.flags[i] & kVectors)
+#pragma unroll 1
+    for (; base + kNumbers <= end; base += kNumbers) update<N, P, G, EIGHT, true>(a, i, base, h, st, factor);
+#pragma unroll 1
+  for (; base < end; base += kNumbers) update<N, P, G, EIGHT, false>(a, i, base, h, st, factor);
+}
 template <int N, typename P, typename G>
-__device__ __forceinline__ void update_typed(const Tensors<N>& a, int i, int64_t base, const Hyper& h, const Step& st,
-                                             float factor) {
-  const bool vectors = a.flags[i] & kVectors && base + kNumbers <= a.count[i];
-  if (a.flags[i] & k8Bits) {
-    if (vectors)
-      update<N, P, G, true, true>(a, i, base, h, st, factor);
-    else
-      update<N, P, G, true, false>(a, i, base, h, st, factor);
-  } else {
-    if (vectors)
-      update<N, P, G, false, true>(a, i, base, h, st, factor);
-    else
-      update<N, P, G, false, false>(a, i, base, h, st, factor);
-  }
+__device__ __forceinline__ void update_typed(const Tensors<N>& a, int i, int64_t base, int64_t end, const Hyper& h,
+                                             const Step& st, float factor) {
+  if (a.flags[i] & k8Bits)
+    update_run<N, P, G, true>(a, i, base, end, h, st, factor);
+  else
+    update_run<N, P, G, false>(a, i, base, end, h, st, factor);
 }
 
 template <int N>
@@ -315,12 +392,13 @@ __global__ void __launch_bounds__(kThreads, kBlocksPerSm)
       k = mix(k + (uint32_t)taken);
       st.key = mix(k ^ a.id[i]);
     }
-    const int64_t base = (task - a.first[i]) * kNumbers;
+    const int64_t base = (task - a.first[i]) * a.numbers, left = a.count[i] - base;
+    const int64_t end = base + (left < a.numbers ? left : a.numbers);
     switch (a.flags[i] & (kParamBf16 | kGradBf16)) {
-      case 0: update_typed<N, float, float>(a, i, base, h, st, factor); break;
-      case kParamBf16: update_typed<N, __nv_bfloat16, float>(a, i, base, h, st, factor); break;
-      case kGradBf16: update_typed<N, float, __nv_bfloat16>(a, i, base, h, st, factor); break;
-      default: update_typed<N, __nv_bfloat16, __nv_bfloat16>(a, i, base, h, st, factor);
+      case 0: update_typed<N, float, float>(a, i, base, end, h, st, factor); break;
+      case kParamBf16: update_typed<N, __nv_bfloat16, float>(a, i, base, end, h, st, factor); break;
+      case kGradBf16: update_typed<N, float, __nv_bfloat16>(a, i, base, end, h, st, factor); break;
+      default: update_typed<N, __nv_bfloat16, __nv_bfloat16>(a, i, base, end, h, st, factor);
     }
   }
   // the last block to come here counts the step: every other one has read the counts
@@ -335,6 +413,31 @@ __global__ void __launch_bounds__(kThreads, kBlocksPerSm)
     for (int k = threadIdx.x; k < a.n; k += kThreads) *a.step[k] += 1;
 }
 
+// Adds the squares of `count` numbers to a lane's four sums.
+template <typename T>
+__device__ __forceinline__ void add_squares(const T* g, int count, bool vectors, int lane, double (&part)[4]) {
+  constexpr int kLoads = 4;
+  if (vectors && count == kNormNumbers) {
+#pragma unroll 1
+    for (int q = 4 * lane; q < kNormNumbers; q += 128 * kLoads) {
+      float v[kLoads][4];
+#pragma unroll
+      for (int u = 0; u < kLoads; ++u) load4<T, true>(g + q + 128 * u, 4, v[u]);
+#pragma unroll
+      for (int u = 0; u < kLoads; ++u)
+#pragma unroll
+        for (int j = 0; j < 4; ++j) part[j] = fma((double)v[u][j], (double)v[u][j], part[j]);
+    }
+    return;
+  }
+  for (int q = 4 * lane; q < count; q += 128) {
+    float v[4];
+    load4<T, false>(g + q, count - q, v);
+#pragma unroll
+    for (int j = 0; j < 4; ++j) part[j] = fma((double)v[j], (double)v[j], part[j]);
+  }
+}
+
 // result = (norm of all gradients, min(1, max_norm / (norm + 1e-6))).  Squares and sums in 64 bits: a gradient of 10^20 is no
 // infinity, and the order is fixed: a block's tasks, then the blocks.
 template <int N>
@@ -343,17 +446,18 @@ __global__ void __launch_bounds__(kThreads)
                      float* result) {
   const int lane = threadIdx.x & 31;
   const int64_t tasks = a.first[a.n];
-  double sum = 0.0;
+  double part[4] = {};
   int i = 0;
   for (int64_t task = (int64_t)blockIdx.x * kWarps + threadIdx.x / 32; task < tasks; task += (int64_t)gridDim.x * kWarps) {
     i = tensor_of(a, task, i);
-    const int64_t base = (task - a.first[i]) * kNumbers;
-    for (int64_t q = base + lane; q < base + kNumbers && q < a.count[i]; q += 32) {
-      const double g = a.flags[i] & kGradBf16 ? (double)__bfloat162float(static_cast<const __nv_bfloat16*>(a.grad[i])[q])
-                                              : (double)static_cast<const float*>(a.grad[i])[q];
-      sum += g * g;
-    }
+    const int64_t base = (task - a.first[i]) * kNormNumbers;
+    const int64_t count = a.count[i] - base < kNormNumbers ? a.count[i] - base : kNormNumbers;
+    if (a.flags[i] & kGradBf16)
+      add_squares(static_cast<const __nv_bfloat16*>(a.grad[i]) + base, (int)count, a.flags[i] & kVectors, lane, part);
+    else
+      add_squares(static_cast<const float*>(a.grad[i]) + base, (int)count, a.flags[i] & kVectors, lane, part);
   }
+  double sum = (part[0] + part[1]) + (part[2] + part[3]);
   __shared__ double sums[kWarps];
   __shared__ bool last;
 #pragma unroll
@@ -396,7 +500,7 @@ bool aligned(const void* p, size_t to) { return (uintptr_t)p % to == 0; }
 
 // The list's tensors from `at` on, as many as fit; returns their tasks.
 template <int N>
-int64_t fill(const dg_adamw_list_t& t, int64_t at, bool gradients_only, Tensors<N>* a) {
+int64_t fill(const dg_adamw_list_t& t, int64_t at, bool gradients_only, int32_t each, Tensors<N>* a) {
   int64_t tasks = 0;
   const int n = t.tensors - at < N ? (int)(t.tensors - at) : N;
   for (int k = 0; k < n; ++k) {
@@ -406,7 +510,7 @@ int64_t fill(const dg_adamw_list_t& t, int64_t at, bool gradients_only, Tensors<
     a->grad[k] = t.grad[i];
     a->count[k] = t.numbers[i];
     a->first[k] = tasks;
-    tasks += (t.numbers[i] + kNumbers - 1) / kNumbers;
+    tasks += (t.numbers[i] + each - 1) / each;
     if (!gradients_only) {
       const bool bf16 = t.param_type[i] == DG_BF16, eight = t.state_bits[i] == 8;
       a->param[k] = t.param[i];
@@ -424,6 +528,7 @@ int64_t fill(const dg_adamw_list_t& t, int64_t at, bool gradients_only, Tensors<
     a->flags[k] = (uint8_t)(flags | (vectors ? kVectors : 0));
   }
   a->first[n] = tasks;
+  a->numbers = each;
   a->n = n;
   return tasks;
 }
@@ -439,7 +544,9 @@ template <int N>
 dg_status_t step_launch(const dg_adamw_list_t& t, int64_t at, const Hyper& h, const float* factor, uint64_t seed, Workspace* ws,
                         int sms, cudaStream_t s) {
   Tensors<N> a;
-  const int64_t tasks = fill(t, at, false, &a);
+  // Long tasks where every warp has some: what a warp finds out about its tensor serves more numbers.
+  int64_t tasks = fill(t, at, false, kNumbers, &a);
+  if (tasks > (int64_t)sms * kBlocksPerSm * kWarps * 2 * kBlocksPerTask) tasks = fill(t, at, false, kNumbers * kBlocksPerTask, &a);
   int64_t blocks = (tasks + kWarps - 1) / kWarps;
   if (blocks > sms * kBlocksPerSm) blocks = sms * kBlocksPerSm;
   if (blocks < 1) blocks = 1;  // tensors without numbers count their steps too
@@ -451,8 +558,11 @@ dg_status_t step_launch(const dg_adamw_list_t& t, int64_t at, const Hyper& h, co
 template <int N>
 dg_status_t norm_launch(const dg_adamw_list_t& t, int64_t at, float max_norm, Workspace* ws, float* result, cudaStream_t s) {
   Tensors<N> a;
-  fill(t, at, true, &a);
-  grad_norm_kernel<N><<<kNormBlocks, kThreads, 0, s>>>(a, at == 0, at + a.n == t.tensors, max_norm, ws, result);
+  const int64_t tasks = fill(t, at, true, kNormNumbers, &a);
+  int64_t blocks = (tasks + kWarps - 1) / kWarps;
+  if (blocks > kNormBlocks || t.tensors > N) blocks = kNormBlocks;  // the launches of one list add to the same sums
+  if (blocks < 1) blocks = 1;
+  grad_norm_kernel<N><<<(unsigned)blocks, kThreads, 0, s>>>(a, at == 0, at + a.n == t.tensors, max_norm, ws, result);
   DG_CUDA(cudaGetLastError());
   count_launches(1);
   return DG_OK;
@@ -516,8 +626,10 @@ extern "C" dg_status_t dg_adamw_step(const dg_adamw_list_t* list, double lr, dou
   if (!(lr >= 0.0 && lr < INFINITY) || !(eps >= 0.0 && eps < INFINITY) || !(weight_decay >= 0.0 && weight_decay < INFINITY))
     return invalid("lr, eps and weight_decay must be finite and not negative");
   if (list->tensors == 0) return DG_OK;
-  const Hyper h{lr, log2(beta1), log2(beta2), (float)(1.0 - beta1), (float)beta2, (float)(1.0 - beta2), (float)eps,
-                (float)(1.0 - lr * weight_decay)};
+  // an eps below the least normal number is that: its inverse has to be finite
+  const float least = eps > 0.0 && eps < (double)kLeastScale ? kLeastScale : (float)eps;
+  const Hyper h{lr, log2(beta1), log2(beta2), (float)beta1, (float)(1.0 - beta1), (float)beta2, (float)(1.0 - beta2), least,
+                (float)(1.0 - lr * weight_decay), (float)sqrt(beta2), (float)sqrt(1.0 - beta2)};
   int sms = 0;
   if (dg_status_t st = device_sms(&sms)) return st;
   Workspace* ws = static_cast<Workspace*>(workspace);
