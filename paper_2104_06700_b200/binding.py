@@ -241,11 +241,12 @@ _data_ptr, _numel, _contiguous = torch.Tensor.data_ptr, torch.Tensor.numel, torc
 _get_device, _dtype = torch.Tensor.get_device, torch.Tensor.dtype.__get__
 
 
-def _check_tensors(tensors, dtypes, device: int, name: str) -> None:
-    """All contiguous, on one device and of one of the types.  The calls take long lists: whole ones are asked, tensor by
-    tensor only to say which one is wrong."""
-    if (device >= 0 and set(map(_dtype, tensors)) <= dtypes and set(map(_get_device, tensors)) <= {device} and all(map(_contiguous, tensors))):
-        return
+def _check_tensors(tensors, dtypes, device: int, name: str) -> list:
+    """The types of tensors that are all contiguous, on one device and of one of the types.  The calls take long lists: whole
+    ones are asked, tensor by tensor only to say which one is wrong."""
+    types = list(map(_dtype, tensors))
+    if dtypes.issuperset(types) and {device}.issuperset(map(_get_device, tensors)) and device >= 0 and all(map(_contiguous, tensors)):
+        return types
     for i, t in enumerate(tensors):
         if t.dtype not in dtypes:
             raise TypeError(f"{name}[{i}] must be {' or '.join(sorted(map(str, dtypes)))}, got {t.dtype}")
@@ -253,6 +254,7 @@ def _check_tensors(tensors, dtypes, device: int, name: str) -> None:
             raise ValueError(f"{name}[{i}] must be a CUDA tensor on the current device, it is on {t.device}")
         if not t.is_contiguous():
             raise ValueError(f"{name}[{i}] must be contiguous")
+    return types
 
 
 def _check_sizes(tensors, numbers, name: str) -> None:
@@ -265,50 +267,69 @@ def _pointers(tensors) -> array:
     return array("Q", map(_data_ptr, tensors))
 
 
-def _codes(tensors) -> array:
-    return array("i", map(_TYPE_CODES.__getitem__, map(_dtype, tensors)))
+_FLOAT_SET, _E4M3_SET, _F32_SET = frozenset(_FLOATS), frozenset([torch.float8_e4m3fn]), frozenset([torch.float32])
 
 
 class AdamwList:
     """A ``dg_adamw_list_t``: parameters with their gradients, states and steps, in lists of one length.  ``scales[i]`` is a
     tensor where the states of parameter i are 8-bit (float8_e4m3fn) and None where they are fp32; ``copies[i]`` a bf16 copy
-    of an fp32 parameter or None.  With gradients alone it serves ``dg_grad_norm``."""
+    of an fp32 parameter or None.  With gradients alone it serves ``dg_grad_norm``.
+
+    A list may serve many steps: the memory of states, steps and scales is kept alive by it; gradients, parameters and copies
+    are named anew by ``refresh`` before each step."""
 
     def __init__(self, grads, params=None, exp_avgs=None, exp_avg_sqs=None, steps=None, scales=None, copies=None, ids=None):
         self.count = len(grads)
-        self._keep = grads      # what a caller made for this list alone has to live until the launch
-        device = _device() if self.count and grads[0].is_cuda else -1
-        _check_tensors(grads, set(_FLOATS), device, "grads")
-        numbers = list(map(_numel, grads))
-        grad_types, grad_pointers = _codes(grads), _pointers(grads)
-        fields = [array("q", numbers), None, grad_pointers, None, None, None, None, None, None, grad_types, None, None]
+        self.device = _device() if self.count and grads[0].is_cuda else -1
+        self._numbers = list(map(_numel, grads))
+        # numbers, param, grad, exp_avg, exp_avg_sq, scales, copy, step, param_type, grad_type, state_bits, id
+        self._fields = fields = [array("q", self._numbers), *[None] * 11]
+        self._types = [None, None]
         if params is not None:
-            for name, tensors, types in (("params", params, set(_FLOATS)), ("steps", steps, {torch.int64})):
-                _check_tensors(tensors, types, device, name)
-            _check_sizes(params, numbers, "params")
+            device = self.device
+            _check_tensors(steps, {torch.int64}, device, "steps")
             _check_sizes(steps, [1] * self.count, "steps")
             eight = [s is not None for s in scales] if scales is not None else [False] * self.count
             for name, tensors in (("exp_avgs", exp_avgs), ("exp_avg_sqs", exp_avg_sqs)):
-                _check_sizes(tensors, numbers, name)
-                _check_tensors([t for t, e in zip(tensors, eight) if e], {torch.float8_e4m3fn}, device, name)
-                _check_tensors([t for t, e in zip(tensors, eight) if not e], {torch.float32}, device, name)
-            fields[1], fields[3:5], fields[7] = _pointers(params), map(_pointers, (exp_avgs, exp_avg_sqs)), _pointers(steps)
-            fields[8] = _codes(params)
+                _check_sizes(tensors, self._numbers, name)
+                _check_tensors([t for t, e in zip(tensors, eight) if e], _E4M3_SET, device, name)
+                _check_tensors([t for t, e in zip(tensors, eight) if not e], _F32_SET, device, name)
+            fields[3:5], fields[7] = map(_pointers, (exp_avgs, exp_avg_sqs)), _pointers(steps)
             fields[10] = array("i", [8 if e else 32 for e in eight])
             fields[11] = array("I", range(self.count) if ids is None else ids)
             if len(fields[11]) != self.count:
                 raise ValueError("ids must be as many as the tensors")
-            if any(eight):
-                some = [s for s in scales if s is not None]
-                _check_tensors(some, {torch.float32}, device, "scales")
-                _check_sizes(some, [2 * ((n + 255) // 256) for n, e in zip(numbers, eight) if e], "scales")
+            some = [s for s in scales if s is not None] if scales is not None else []
+            if some:
+                _check_tensors(some, _F32_SET, device, "scales")
+                _check_sizes(some, [2 * ((n + 255) // 256) for n, e in zip(self._numbers, eight) if e], "scales")
                 fields[5] = array("Q", [0 if s is None else s.data_ptr() for s in scales])
-            if copies is not None and any(c is not None for c in copies):
-                some = [c for c in copies if c is not None]
-                _check_tensors(some, {torch.bfloat16}, device, "copies")
-                _check_sizes(some, [n for n, c in zip(numbers, copies) if c is not None], "copies")
-                fields[6] = array("Q", [0 if c is None else c.data_ptr() for c in copies])
-        self._fields = fields
+            self._storages = [t.untyped_storage() for t in (*exp_avgs, *exp_avg_sqs, *steps, *some)]
+        self.refresh(grads, params, copies)
+
+    def forget_gradients(self) -> None:
+        """Once the calls are queued: a list that is kept must not keep a step's gradients."""
+        self._keep = None
+
+    def refresh(self, grads, params=None, copies=None) -> None:
+        """Names (and checks) what may lie elsewhere at every step."""
+        fields = self._fields
+        self._keep = grads      # what a caller made for this step alone has to live until the launch
+        for at, type_at, name, tensors in ((2, 9, "grads", grads), (1, 8, "params", params)):
+            if tensors is not None:
+                types = _check_tensors(tensors, _FLOAT_SET, self.device, name)
+                if types != self._types[at - 1]:
+                    fields[type_at] = array("i", map(_TYPE_CODES.__getitem__, types))
+                    self._types[at - 1] = types
+                _check_sizes(tensors, self._numbers, name)
+                fields[at] = _pointers(tensors)
+        if copies is not None and any(c is not None for c in copies):
+            some = [c for c in copies if c is not None]
+            _check_tensors(some, {torch.bfloat16}, self.device, "copies")
+            _check_sizes(some, [n for n, c in zip(self._numbers, copies) if c is not None], "copies")
+            fields[6] = array("Q", [0 if c is None else c.data_ptr() for c in copies])
+        else:
+            fields[6] = None
         self.struct = struct.pack("q12Q", self.count, *[0 if f is None else f.buffer_info()[0] for f in fields])
 
 
@@ -319,16 +340,15 @@ def adamw_workspace(device) -> torch.Tensor:
 
 def _workspace_ptr(workspace):
     _has(workspace, DG_ADAMW_WORKSPACE_BYTES, "workspace")
-    _on_current_device(workspace=workspace)
     return _dev_ptr(workspace, torch.uint8, "workspace")
 
 
 def dg_grad_norm(tensors: AdamwList, max_norm: float, workspace: torch.Tensor, result: torch.Tensor, stream=None) -> torch.Tensor:
     """Wraps ``dg_grad_norm``: result (2 fp32) = (norm of all gradients, min(1, max_norm / (norm + 1e-6)))."""
     _has(result, 2, "result")
-    _on_current_device(result=result)
-    _check(lib().dg_grad_norm(tensors.struct, float(max_norm), _workspace_ptr(workspace),
-                              _dev_ptr(result, torch.float32, "result"), _stream(stream)))
+    _on_current_device(result=result, workspace=workspace)
+    _check(lib().dg_grad_norm(tensors.struct, max_norm, _workspace_ptr(workspace), _dev_ptr(result, torch.float32, "result"),
+                              _stream(stream)))
     return result
 
 
@@ -336,7 +356,7 @@ def dg_adamw_step(tensors: AdamwList, lr: float, beta1: float, beta2: float, eps
                   workspace: torch.Tensor, grad_factor: Optional[torch.Tensor] = None, seed: int = 0, stream=None) -> None:
     """Wraps ``dg_adamw_step``: updates the tensors, their states and their steps in place."""
     _has(grad_factor, 1, "grad_factor")
-    _on_current_device(grad_factor=grad_factor)
+    _on_current_device(grad_factor=grad_factor, workspace=workspace)
     _check(lib().dg_adamw_step(tensors.struct, lr, beta1, beta2, eps, weight_decay,
                                _dev_ptr(grad_factor, torch.float32, "grad_factor"), seed & 0xffffffffffffffff,
                                _workspace_ptr(workspace), _stream(stream)))

@@ -8,6 +8,8 @@
 #include <cuda_bf16.h>
 #include <math.h>
 
+#include <type_traits>
+
 #include "dg_internal.cuh"
 
 namespace dg {
@@ -15,7 +17,10 @@ namespace {
 
 constexpr int kThreads = 256;
 constexpr int kWarps = kThreads / 32;
-constexpr int kBlocksPerSm = 3;                     // what 80 registers a thread leave room for
+// Blocks of an SM.  Numbers in 32 bits: two, whose 128 registers a thread hold a task's first block while the powers of beta
+// are on their way (245 M numbers: 1042 us, three blocks 1100).  In 8 bits arithmetic counts, and more warps hide it: four
+// at 64 registers (698 us; three 715, two 806, two that load a block ahead 743).
+constexpr int blocks_per_sm(bool eight) { return eight ? 4 : 2; }
 constexpr int kNumbers = 256;                       // of a warp's task: 8 a lane, and one scale
 constexpr int kBlocksPerTask = 4;
 constexpr int kNormNumbers = 2048;                  // of a warp's task of the norm
@@ -75,24 +80,32 @@ __device__ __forceinline__ int tensor_of(const Tensors<N>& a, int64_t task, int 
   return lo;
 }
 
-// Four neighbouring numbers; `left` of them exist.
+// Four neighbouring numbers as they are stored; `left` of them exist.
+template <typename T>
+struct Quad {
+  std::conditional_t<sizeof(T) == 4, float4, uint2> raw;
+};
 template <typename T, bool VEC>
-__device__ __forceinline__ void load4(const T* p, int left, float* out) {
-  if constexpr (VEC && sizeof(T) == 4) {
-    const float4 q = *reinterpret_cast<const float4*>(p);
-    out[0] = q.x, out[1] = q.y, out[2] = q.z, out[3] = q.w;
-  } else if constexpr (VEC) {
-    const uint2 q = *reinterpret_cast<const uint2*>(p);
-    out[0] = __uint_as_float(q.x << 16), out[1] = __uint_as_float(q.x & 0xffff0000u);
-    out[2] = __uint_as_float(q.y << 16), out[3] = __uint_as_float(q.y & 0xffff0000u);
+__device__ __forceinline__ Quad<T> load4(const T* p, int left) {
+  Quad<T> r;
+  if constexpr (VEC) {
+    r.raw = *reinterpret_cast<const decltype(r.raw)*>(p);
+  } else if constexpr (sizeof(T) == 4) {
+    r.raw = make_float4(left > 0 ? p[0] : 0.f, left > 1 ? p[1] : 0.f, left > 2 ? p[2] : 0.f, left > 3 ? p[3] : 0.f);
   } else {
-#pragma unroll
-    for (int j = 0; j < 4; ++j) {
-      out[j] = 0.f;
-      if (j < left) {
-        if constexpr (sizeof(T) == 4) out[j] = p[j]; else out[j] = __bfloat162float(p[j]);
-      }
-    }
+    const uint16_t* h = reinterpret_cast<const uint16_t*>(p);
+    r.raw = make_uint2((left > 0 ? h[0] : 0u) | (left > 1 ? (uint32_t)h[1] << 16 : 0u),
+                       (left > 2 ? h[2] : 0u) | (left > 3 ? (uint32_t)h[3] << 16 : 0u));
+  }
+  return r;
+}
+template <typename T>
+__device__ __forceinline__ void numbers_of(const Quad<T>& q, float* out) {
+  if constexpr (sizeof(T) == 4) {
+    out[0] = q.raw.x, out[1] = q.raw.y, out[2] = q.raw.z, out[3] = q.raw.w;
+  } else {
+    out[0] = __uint_as_float(q.raw.x << 16), out[1] = __uint_as_float(q.raw.x & 0xffff0000u);
+    out[2] = __uint_as_float(q.raw.y << 16), out[3] = __uint_as_float(q.raw.y & 0xffff0000u);
   }
 }
 template <bool VEC>
@@ -240,45 +253,68 @@ __device__ __forceinline__ void store_param(const Tensors<N>& a, int i, int64_t 
   }
 }
 
-// One task: the numbers base .. base + 255 of a tensor, as far as it goes.  A lane has four at 4 lane, four 128 further.
-template <int N, typename P, typename G, bool EIGHT, bool VEC>
-__device__ __forceinline__ void update(const Tensors<N>& a, int i, int64_t base, const Hyper& h, const Step& st, float factor) {
+// The numbers base .. base + 255 of a tensor, as far as it goes, as they are stored.  A lane has four at 4 lane, four 128
+// further.
+template <typename P, typename G, bool EIGHT>
+struct Block {
+  Quad<P> p[2];
+  Quad<G> g[2];
+  std::conditional_t<EIGHT, uint32_t, Quad<float>> m[2], v[2];
+  float2 scale;
+};
+__device__ __forceinline__ int left_of(int64_t q, int64_t end) { return (int)(end - q < 0 ? 0 : end - q < 4 ? end - q : 4); }
+
+template <typename P, typename G, bool EIGHT, bool VEC, int N>
+__device__ __forceinline__ Block<P, G, EIGHT> load_block(const Tensors<N>& a, int i, int64_t base) {
+  Block<P, G, EIGHT> r;
+#pragma unroll
+  for (int k = 0; k < 2; ++k) {
+    const int64_t q = base + 4 * (threadIdx.x & 31) + 128 * k;
+    const int left = VEC ? 4 : left_of(q, a.count[i]);
+    r.p[k] = load4<P, VEC>(static_cast<const P*>(a.param[i]) + q, left);
+    r.g[k] = load4<G, VEC>(static_cast<const G*>(a.grad[i]) + q, left);
+    if constexpr (EIGHT) {
+      r.m[k] = load_bytes<VEC>(static_cast<const uint8_t*>(a.m[i]) + q, left);
+      r.v[k] = load_bytes<VEC>(static_cast<const uint8_t*>(a.v[i]) + q, left);
+    } else {
+      r.m[k] = load4<float, VEC>(static_cast<const float*>(a.m[i]) + q, left);
+      r.v[k] = load4<float, VEC>(static_cast<const float*>(a.v[i]) + q, left);
+    }
+  }
+  if constexpr (EIGHT) r.scale = a.scales[i][base / kNumbers];
+  return r;
+}
+
+template <typename P, typename G, bool EIGHT, bool VEC, int N>
+__device__ __forceinline__ void update(const Tensors<N>& a, int i, int64_t base, const Block<P, G, EIGHT>& in, const Hyper& h,
+                                       const Step& st, float factor) {
   const int lane = threadIdx.x & 31;
   const int64_t at = base + 4 * lane, end = a.count[i];
   const uint32_t key = mix(st.key ^ (uint32_t)(base >> 32));
   float p[8], g[8], m[8], v[8];   // EIGHT: v is sqrt(v)
-  Two m2[4], u2[4];
-  float2 scale = make_float2(0.f, 0.f);
-  if (EIGHT) scale = a.scales[i][base / kNumbers];
 #pragma unroll
   for (int k = 0; k < 2; ++k) {
-    const int64_t q = at + 128 * k;
-    const int left = VEC ? 4 : (int)(end - q < 0 ? 0 : end - q < 4 ? end - q : 4);
-    load4<P, VEC>(static_cast<const P*>(a.param[i]) + q, left, p + 4 * k);
-    load4<G, VEC>(static_cast<const G*>(a.grad[i]) + q, left, g + 4 * k);
-    if constexpr (EIGHT) {
-      const uint32_t mb = load_bytes<VEC>(static_cast<const uint8_t*>(a.m[i]) + q, left);
-      const uint32_t ub = load_bytes<VEC>(static_cast<const uint8_t*>(a.v[i]) + q, left);
-      m2[2 * k] = from_e4m3(mb), m2[2 * k + 1] = from_e4m3(mb >> 16);
-      u2[2 * k] = from_e4m3(ub), u2[2 * k + 1] = from_e4m3(ub >> 16);
-    } else {
-      load4<float, VEC>(static_cast<const float*>(a.m[i]) + q, left, m + 4 * k);
-      load4<float, VEC>(static_cast<const float*>(a.v[i]) + q, left, v + 4 * k);
+    numbers_of(in.p[k], p + 4 * k);
+    numbers_of(in.g[k], g + 4 * k);
+    if constexpr (!EIGHT) {
+      numbers_of(in.m[k], m + 4 * k);
+      numbers_of(in.v[k], v + 4 * k);
     }
   }
   if constexpr (EIGHT) {
     // scales and betas in one factor of each code
-    const Two keep_m = both(h.beta1 * scale.x), keep_u = both(h.root2 * scale.y);
+    const Two keep_m = both(h.beta1 * in.scale.x), keep_u = both(h.root2 * in.scale.y);
     const Two take_m = both(h.rest1 * factor), take_u = both(h.root_rest2 * factor);
     float most_m = 0.f, most_u = 0.f;
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
-      const Two gj = two(g[2 * j], g[2 * j + 1]), old = u2[j] * keep_u, now = gj * take_u;
-      m2[j] = fma2(m2[j], keep_m, gj * take_m);
-      const float2 vj = apart(fma2(old, old, now * now)), mj = apart(m2[j]);
+      const Two gj = two(g[2 * j], g[2 * j + 1]), now = gj * take_u;
+      const Two old = from_e4m3(in.v[j / 2] >> (16 * (j % 2))) * keep_u;
+      const Two mean = fma2(from_e4m3(in.m[j / 2] >> (16 * (j % 2))), keep_m, gj * take_m);
+      const float2 vj = apart(fma2(old, old, now * now)), mj = apart(mean);
       v[2 * j] = fast_sqrt(vj.x), v[2 * j + 1] = fast_sqrt(vj.y);
       const float2 under = apart(fma2(two(v[2 * j], v[2 * j + 1]), both(st.c2), both(h.eps)));
-      const Two ratio = m2[j] * two(fast_inverse(under.x), fast_inverse(under.y));
+      const Two ratio = mean * two(fast_inverse(under.x), fast_inverse(under.y));
       const float2 pj = apart(fma2(ratio, both(-st.c1), two(p[2 * j], p[2 * j + 1]) * both(h.decay)));
       p[2 * j] = pj.x, p[2 * j + 1] = pj.y;
       m[2 * j] = mj.x, m[2 * j + 1] = mj.y;
@@ -292,8 +328,7 @@ __device__ __forceinline__ void update(const Tensors<N>& a, int i, int64_t base,
       most_m = warp_most_finite(m);
       most_u = warp_most_finite(v);
     }
-    scale.x = fmaxf(__fdiv_rn(most_m, kLargest), kLeastScale);
-    scale.y = fmaxf(__fdiv_rn(most_u, kLargest), kLeastScale);
+    const float2 scale = make_float2(fmaxf(__fdiv_rn(most_m, kLargest), kLeastScale), fmaxf(__fdiv_rn(most_u, kLargest), kLeastScale));
     if (lane == 0) a.scales[i][base / kNumbers] = scale;
     const Two inv_m = both(__frcp_rn(scale.x)), inv_u = both(__frcp_rn(scale.y)), front = both(0x1p-120f);
     float ym[8], yu[8];
@@ -306,7 +341,7 @@ __device__ __forceinline__ void update(const Tensors<N>& a, int i, int64_t base,
 #pragma unroll
     for (int k = 0; k < 2; ++k) {
       const int64_t q = at + 128 * k;
-      const int left = VEC ? 4 : (int)(end - q < 0 ? 0 : end - q < 4 ? end - q : 4);
+      const int left = VEC ? 4 : left_of(q, end);
       uint32_t r[4], cm[4], cu[4];
 #pragma unroll
       for (int j = 0; j < 4; ++j) {
@@ -336,7 +371,7 @@ __device__ __forceinline__ void update(const Tensors<N>& a, int i, int64_t base,
 #pragma unroll
     for (int k = 0; k < 2; ++k) {
       const int64_t q = at + 128 * k;
-      const int left = VEC ? 4 : (int)(end - q < 0 ? 0 : end - q < 4 ? end - q : 4);
+      const int left = VEC ? 4 : left_of(q, end);
       uint32_t r[4] = {};
       if (sizeof(P) == 2) {
 #pragma unroll
@@ -350,25 +385,7 @@ __device__ __forceinline__ void update(const Tensors<N>& a, int i, int64_t base,
 }
 
 template <int N, typename P, typename G, bool EIGHT>
-__device__ __forceinline__ void update_run(const Tensors<N>& a, int i, int64_t base, int64_t end, const Hyper& h, const Step& st,
-                                           float factor) {
-  if (a.flags[i] & kVectors)
-#pragma unroll 1
-    for (; base + kNumbers <= end; base += kNumbers) update<N, P, G, EIGHT, true>(a, i, base, h, st, factor);
-#pragma unroll 1
-  for (; base < end; base += kNumbers) update<N, P, G, EIGHT, false>(a, i, base, h, st, factor);
-}
-template <int N, typename P, typename G>
-__device__ __forceinline__ void update_typed(const Tensors<N>& a, int i, int64_t base, int64_t end, const Hyper& h,
-                                             const Step& st, float factor) {
-  if (a.flags[i] & k8Bits)
-    update_run<N, P, G, true>(a, i, base, end, h, st, factor);
-  else
-    update_run<N, P, G, false>(a, i, base, end, h, st, factor);
-}
-
-template <int N>
-__global__ void __launch_bounds__(kThreads, kBlocksPerSm)
+__global__ void __launch_bounds__(kThreads, blocks_per_sm(EIGHT))
     adamw_kernel(const __grid_constant__ Tensors<N> a, Hyper h, const float* factor_at, uint64_t seed, Workspace* ws) {
   const int lane = threadIdx.x & 31;
   cudaGridDependencySynchronize();
@@ -378,6 +395,11 @@ __global__ void __launch_bounds__(kThreads, kBlocksPerSm)
   Step st{};
   for (int64_t task = (int64_t)blockIdx.x * kWarps + threadIdx.x / 32; task < tasks; task += (int64_t)gridDim.x * kWarps) {
     const int now = tensor_of(a, task, i < 0 ? 0 : i);
+    int64_t base = (task - a.first[now]) * a.numbers;
+    const int64_t left = a.count[now] - base, end = base + (left < a.numbers ? left : a.numbers);
+    const bool vectors = a.flags[now] & kVectors && base + kNumbers <= end;
+    Block<P, G, EIGHT> first;
+    if (!EIGHT && vectors) first = load_block<P, G, EIGHT, true>(a, now, base);
     if (now != i) {
       i = now;
       const int64_t taken = *a.step[i];
@@ -392,14 +414,18 @@ __global__ void __launch_bounds__(kThreads, kBlocksPerSm)
       k = mix(k + (uint32_t)taken);
       st.key = mix(k ^ a.id[i]);
     }
-    const int64_t base = (task - a.first[i]) * a.numbers, left = a.count[i] - base;
-    const int64_t end = base + (left < a.numbers ? left : a.numbers);
-    switch (a.flags[i] & (kParamBf16 | kGradBf16)) {
-      case 0: update_typed<N, float, float>(a, i, base, end, h, st, factor); break;
-      case kParamBf16: update_typed<N, __nv_bfloat16, float>(a, i, base, end, h, st, factor); break;
-      case kGradBf16: update_typed<N, float, __nv_bfloat16>(a, i, base, end, h, st, factor); break;
-      default: update_typed<N, __nv_bfloat16, __nv_bfloat16>(a, i, base, end, h, st, factor);
+    if (vectors) {
+      if (!EIGHT) {
+        update<P, G, EIGHT, true>(a, i, base, first, h, st, factor);
+        base += kNumbers;
+      }
+#pragma unroll 1
+      for (; base + kNumbers <= end; base += kNumbers)
+        update<P, G, EIGHT, true>(a, i, base, load_block<P, G, EIGHT, true>(a, i, base), h, st, factor);
     }
+#pragma unroll 1
+    for (; base < end; base += kNumbers)
+      update<P, G, EIGHT, false>(a, i, base, load_block<P, G, EIGHT, false>(a, i, base), h, st, factor);
   }
   // the last block to come here counts the step: every other one has read the counts
   __shared__ bool last;
@@ -422,7 +448,7 @@ __device__ __forceinline__ void add_squares(const T* g, int count, bool vectors,
     for (int q = 4 * lane; q < kNormNumbers; q += 128 * kLoads) {
       float v[kLoads][4];
 #pragma unroll
-      for (int u = 0; u < kLoads; ++u) load4<T, true>(g + q + 128 * u, 4, v[u]);
+      for (int u = 0; u < kLoads; ++u) numbers_of(load4<T, true>(g + q + 128 * u, 4), v[u]);
 #pragma unroll
       for (int u = 0; u < kLoads; ++u)
 #pragma unroll
@@ -432,7 +458,7 @@ __device__ __forceinline__ void add_squares(const T* g, int count, bool vectors,
   }
   for (int q = 4 * lane; q < count; q += 128) {
     float v[4];
-    load4<T, false>(g + q, count - q, v);
+    numbers_of(load4<T, false>(g + q, count - q), v);
 #pragma unroll
     for (int j = 0; j < 4; ++j) part[j] = fma((double)v[j], (double)v[j], part[j]);
   }
@@ -498,38 +524,43 @@ dg_status_t invalid(const char* msg) {
 
 bool aligned(const void* p, size_t to) { return (uintptr_t)p % to == 0; }
 
-// The list's tensors from `at` on, as many as fit; returns their tasks.
+// Which kernel takes a tensor; the norm's takes all gradients.
+int kind_of(const dg_adamw_list_t& t, int64_t i) {
+  return (t.param_type[i] == DG_BF16 ? kParamBf16 : 0) | (t.grad_type[i] == DG_BF16 ? kGradBf16 : 0) | (t.state_bits[i] == 8 ? k8Bits : 0);
+}
+
+// The list's tensors from *at on, of one kind (-1: gradients alone, of any), as many as fit; *at goes behind them.  Returns
+// their tasks of `each` numbers.
 template <int N>
-int64_t fill(const dg_adamw_list_t& t, int64_t at, bool gradients_only, int32_t each, Tensors<N>* a) {
+int64_t fill(const dg_adamw_list_t& t, int64_t* at, int kind, int32_t each, Tensors<N>* a) {
   int64_t tasks = 0;
-  const int n = t.tensors - at < N ? (int)(t.tensors - at) : N;
-  for (int k = 0; k < n; ++k) {
-    const int64_t i = at + k;
-    int flags = t.grad_type[i] == DG_BF16 ? kGradBf16 : 0;
+  int k = 0;
+  for (; *at < t.tensors && k < N; ++*at) {
+    const int64_t i = *at;
+    if (kind >= 0 && kind_of(t, i) != kind) continue;
     bool vectors = aligned(t.grad[i], t.grad_type[i] == DG_BF16 ? 8 : 16);
     a->grad[k] = t.grad[i];
     a->count[k] = t.numbers[i];
     a->first[k] = tasks;
     tasks += (t.numbers[i] + each - 1) / each;
-    if (!gradients_only) {
-      const bool bf16 = t.param_type[i] == DG_BF16, eight = t.state_bits[i] == 8;
+    if (kind >= 0) {
       a->param[k] = t.param[i];
       a->m[k] = t.exp_avg[i];
       a->v[k] = t.exp_avg_sq[i];
-      a->scales[k] = eight ? reinterpret_cast<float2*>(t.scales[i]) : nullptr;
+      a->scales[k] = kind & k8Bits ? reinterpret_cast<float2*>(t.scales[i]) : nullptr;
       a->copy[k] = t.copy ? static_cast<__nv_bfloat16*>(t.copy[i]) : nullptr;
       a->step[k] = t.step[i];
       a->id[k] = t.id ? t.id[i] : (uint32_t)i;
-      flags |= (bf16 ? kParamBf16 : 0) | (eight ? k8Bits : 0);
-      const size_t state = eight ? 4 : 16;
-      vectors = vectors && aligned(t.param[i], bf16 ? 8 : 16) && aligned(t.exp_avg[i], state) &&
+      const size_t state = kind & k8Bits ? 4 : 16;
+      vectors = vectors && aligned(t.param[i], kind & kParamBf16 ? 8 : 16) && aligned(t.exp_avg[i], state) &&
                 aligned(t.exp_avg_sq[i], state) && aligned(a->copy[k], 8);
     }
-    a->flags[k] = (uint8_t)(flags | (vectors ? kVectors : 0));
+    a->flags[k] = (uint8_t)((t.grad_type[i] == DG_BF16 ? kGradBf16 : 0) | (vectors ? kVectors : 0));
+    ++k;
   }
-  a->first[n] = tasks;
+  a->first[k] = tasks;
   a->numbers = each;
-  a->n = n;
+  a->n = k;
   return tasks;
 }
 
@@ -540,29 +571,63 @@ dg_status_t device_sms(int* sms) {
   return DG_OK;
 }
 
+struct StepCall {
+  Hyper h;
+  const float* factor;
+  uint64_t seed;
+  Workspace* ws;
+  int sms;
+  cudaStream_t s;
+};
+
+template <int N, typename P, typename G, bool EIGHT>
+dg_status_t step_kind(const dg_adamw_list_t& t, int kind, const StepCall& c) {
+  for (int64_t at = 0; at < t.tensors;) {
+    Tensors<N> a;
+    const int64_t from = at;
+    int64_t tasks = fill(t, &at, kind, kNumbers, &a);
+    if (a.n == 0) break;
+    const int64_t warps = (int64_t)c.sms * blocks_per_sm(EIGHT) * kWarps;
+    // Long tasks where every warp has some: what a warp finds out about its tensor serves more numbers.
+    if (tasks > warps * 2 * kBlocksPerTask) tasks = fill(t, &(at = from), kind, kNumbers * kBlocksPerTask, &a);
+    int64_t blocks = (tasks + kWarps - 1) / kWarps;
+    if (blocks > c.sms * blocks_per_sm(EIGHT)) blocks = c.sms * blocks_per_sm(EIGHT);
+    if (blocks < 1) blocks = 1;  // tensors without numbers count their steps too
+    DG_CUDA(launch_kernel(adamw_kernel<N, P, G, EIGHT>, dim3((unsigned)blocks), kThreads, c.s, true, a, c.h, c.factor, c.seed, c.ws));
+    count_launches(1);
+  }
+  return DG_OK;
+}
+
+// One launch for each kind of tensor in the list: a kernel for all kinds keeps the registers of the dearest for every one.
 template <int N>
-dg_status_t step_launch(const dg_adamw_list_t& t, int64_t at, const Hyper& h, const float* factor, uint64_t seed, Workspace* ws,
-                        int sms, cudaStream_t s) {
-  Tensors<N> a;
-  // Long tasks where every warp has some: what a warp finds out about its tensor serves more numbers.
-  int64_t tasks = fill(t, at, false, kNumbers, &a);
-  if (tasks > (int64_t)sms * kBlocksPerSm * kWarps * 2 * kBlocksPerTask) tasks = fill(t, at, false, kNumbers * kBlocksPerTask, &a);
-  int64_t blocks = (tasks + kWarps - 1) / kWarps;
-  if (blocks > sms * kBlocksPerSm) blocks = sms * kBlocksPerSm;
-  if (blocks < 1) blocks = 1;  // tensors without numbers count their steps too
-  DG_CUDA(launch_kernel(adamw_kernel<N>, dim3((unsigned)blocks), kThreads, s, true, a, h, factor, seed, ws));
-  count_launches(1);
+dg_status_t step_all(const dg_adamw_list_t& t, const StepCall& c) {
+  int kinds = 0;
+  for (int64_t i = 0; i < t.tensors; ++i) kinds |= 1 << kind_of(t, i);
+  for (int kind = 0; kind < 8; ++kind) {
+    if (!(kinds >> kind & 1)) continue;
+    auto typed = [&](auto p, auto g) {
+      using P = decltype(p);
+      using G = decltype(g);
+      return kind & k8Bits ? step_kind<N, P, G, true>(t, kind, c) : step_kind<N, P, G, false>(t, kind, c);
+    };
+    const bool gb = kind & kGradBf16;
+    const dg_status_t st = kind & kParamBf16 ? (gb ? typed(__nv_bfloat16(), __nv_bfloat16()) : typed(__nv_bfloat16(), 0.f))
+                                             : (gb ? typed(0.f, __nv_bfloat16()) : typed(0.f, 0.f));
+    if (st != DG_OK) return st;
+  }
   return DG_OK;
 }
 
 template <int N>
-dg_status_t norm_launch(const dg_adamw_list_t& t, int64_t at, float max_norm, Workspace* ws, float* result, cudaStream_t s) {
+dg_status_t norm_launch(const dg_adamw_list_t& t, int64_t* at, float max_norm, Workspace* ws, float* result, cudaStream_t s) {
   Tensors<N> a;
-  const int64_t tasks = fill(t, at, true, kNormNumbers, &a);
+  const bool first = *at == 0;
+  const int64_t tasks = fill(t, at, -1, kNormNumbers, &a);
   int64_t blocks = (tasks + kWarps - 1) / kWarps;
   if (blocks > kNormBlocks || t.tensors > N) blocks = kNormBlocks;  // the launches of one list add to the same sums
   if (blocks < 1) blocks = 1;
-  grad_norm_kernel<N><<<(unsigned)blocks, kThreads, 0, s>>>(a, at == 0, at + a.n == t.tensors, max_norm, ws, result);
+  grad_norm_kernel<N><<<(unsigned)blocks, kThreads, 0, s>>>(a, first, *at == t.tensors, max_norm, ws, result);
   DG_CUDA(cudaGetLastError());
   count_launches(1);
   return DG_OK;
@@ -612,9 +677,10 @@ extern "C" dg_status_t dg_grad_norm(const dg_adamw_list_t* list, float max_norm,
   if (!result) return invalid("result is NULL");
   Workspace* ws = static_cast<Workspace*>(workspace);
   cudaStream_t s = (cudaStream_t)stream;
-  if (list->tensors <= kFew) return norm_launch<kFew>(*list, 0, max_norm, ws, result, s);
-  for (int64_t i = 0; i < list->tensors; i += kMost)
-    if (dg_status_t st = norm_launch<kMost>(*list, i, max_norm, ws, result, s)) return st;
+  int64_t at = 0;
+  if (list->tensors <= kFew) return norm_launch<kFew>(*list, &at, max_norm, ws, result, s);
+  while (at < list->tensors)
+    if (dg_status_t st = norm_launch<kMost>(*list, &at, max_norm, ws, result, s)) return st;
   return DG_OK;
 }
 
@@ -632,10 +698,6 @@ extern "C" dg_status_t dg_adamw_step(const dg_adamw_list_t* list, double lr, dou
                 (float)(1.0 - lr * weight_decay), (float)sqrt(beta2), (float)sqrt(1.0 - beta2)};
   int sms = 0;
   if (dg_status_t st = device_sms(&sms)) return st;
-  Workspace* ws = static_cast<Workspace*>(workspace);
-  cudaStream_t s = (cudaStream_t)stream;
-  if (list->tensors <= kFew) return step_launch<kFew>(*list, 0, h, grad_factor, seed, ws, sms, s);
-  for (int64_t i = 0; i < list->tensors; i += kMost)
-    if (dg_status_t st = step_launch<kMost>(*list, i, h, grad_factor, seed, ws, sms, s)) return st;
-  return DG_OK;
+  const StepCall c{h, grad_factor, seed, static_cast<Workspace*>(workspace), sms, (cudaStream_t)stream};
+  return list->tensors <= kFew ? step_all<kFew>(*list, c) : step_all<kMost>(*list, c);
 }

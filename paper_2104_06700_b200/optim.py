@@ -2,11 +2,16 @@
 (dg_adamw_step and dg_grad_norm), behind torch's optimiser interface."""
 from __future__ import annotations
 
+import itertools
+import operator
 from typing import Optional
 
 import torch
 
 from . import binding
+
+
+_NONE = itertools.repeat(None)
 
 
 class AdamW(torch.optim.Optimizer):
@@ -37,6 +42,7 @@ class AdamW(torch.optim.Optimizer):
             raise ValueError(f"betas must be in [0, 1), got {betas}")
         self.max_norm, self.grad_norm = max_norm, None
         self._workspace = self._result = None
+        self._tables = {}
         super().__init__(params, dict(lr=lr, betas=betas, eps=eps, weight_decay=weight_decay, state_bits=state_bits,
                                       min_8bit_size=min_8bit_size, master_weights=master_weights, seed=seed))
 
@@ -54,6 +60,7 @@ class AdamW(torch.optim.Optimizer):
         super().__setstate__(state)
         self.__dict__.setdefault("max_norm", None)
         self.grad_norm = self._workspace = self._result = None
+        self._tables = {}
 
     def load_state_dict(self, state_dict) -> None:
         """torch's would cast every state to its parameter's type."""
@@ -82,23 +89,43 @@ class AdamW(torch.optim.Optimizer):
             state["master"] = p.detach().float()
         return state
 
-    def _take(self, group, first: int, lists) -> None:
-        """Adds the group's tensors to the lists; the random bits of the i-th go by first + i."""
-        for i, p in enumerate(group["params"], first):
-            g = p.grad
-            if g is None:
-                continue
-            if g.is_sparse:
-                raise ValueError("sparse gradients are not supported")
-            s = self.state[p]
-            if not s:
-                s.update(self._new_state(p, group))
-            master = s.get("master")
-            # a gradient in another order: the copy lives until the launch, then the allocator's stream order serves
-            row = (g if g.is_contiguous() else g.contiguous(), p if master is None else master, s["exp_avg"], s["exp_avg_sq"],
-                   s["step"], s.get("scales"), None if master is None else p, i)
-            for column, value in zip(lists, row):
-                column.append(value)
+    def _table(self, at: int, group, first: int):
+        """(gradients, the library's list) of the group's parameters that have one; the random bits of the i-th go by first + i.
+        The list is made anew when any of its parameters or states is another tensor than in the last step."""
+        ids, params = range(first, first + len(group["params"])), group["params"]
+        grads = [p.grad for p in params]
+        if any(map(operator.is_, grads, _NONE)):
+            some = [(i, p, g) for i, p, g in zip(ids, params, grads) if g is not None]
+            if not some:
+                return None
+            ids, params, grads = zip(*some)
+        states = [self.state[p] for p in params]
+        if not all(states):
+            for p, s in zip(params, states):
+                if not s:
+                    s.update(self._new_state(p, group))
+        if any(g.layout is not torch.strided for g in grads):
+            raise ValueError("sparse gradients are not supported")
+        if not all(map(torch.Tensor.is_contiguous, grads)):
+            grads = [g.contiguous() for g in grads]      # copies live until the launch, then the allocator's stream order serves
+        columns = [[s["exp_avg"] for s in states], [s["exp_avg_sq"] for s in states], [s["step"] for s in states],
+                   [s.get("scales") for s in states]]
+        masters = [s.get("master") for s in states]
+        copies = None
+        if not all(map(operator.is_, masters, _NONE)):
+            targets = [p if m is None else m for p, m in zip(params, masters)]
+            copies = [None if m is None else p for p, m in zip(params, masters)]
+        else:
+            targets = params
+        known = self._tables.get(at)
+        same = known is not None and len(known[0]) == len(params) and all(map(operator.is_, known[0], params)) and all(
+            all(map(operator.is_, k, c)) for k, c in zip(known[1], columns))
+        if same:
+            known[2].refresh(grads, targets, copies)
+        else:
+            table = binding.AdamwList(grads, targets, *columns, copies, ids)
+            known = self._tables[at] = (list(params), columns, table)
+        return grads, known[2]
 
     @torch.no_grad()
     def step(self, closure=None):
@@ -106,35 +133,38 @@ class AdamW(torch.optim.Optimizer):
         if closure is not None:
             with torch.enable_grad():
                 loss = closure()
-        parts, first = [], 0
-        for group in self.param_groups:
-            lists = [[] for _ in range(8)]
-            self._take(group, first, lists)
-            first += len(group["params"])
-            if lists[0]:
-                parts.append((group, lists))
-        if parts:
-            device = parts[0][1][0][0].device
-            if device.index == torch.cuda.current_device():
-                self._launch(parts, device)
-            else:
-                with torch.cuda.device(device):
-                    self._launch(parts, device)
+        device = next((p.device for group in self.param_groups for p in group["params"] if p.grad is not None), None)
+        if device is None:
+            return loss
+        if device.type != "cuda":
+            raise ValueError("parameters must be contiguous fp32 or bf16 CUDA tensors")
+        if device.index == torch.cuda.current_device():
+            self._launch(device)
+        else:
+            with torch.cuda.device(device):
+                self._launch(device)
         return loss
 
-    def _launch(self, parts, device) -> None:
-        tables = [binding.AdamwList(*lists) for _, lists in parts]
+    def _launch(self, device) -> None:
+        parts, first = [], 0
+        for at, group in enumerate(self.param_groups):
+            table = self._table(at, group, first)
+            first += len(group["params"])
+            if table is not None:
+                parts.append((group, *table))
         if self._workspace is None or self._workspace.device != device:
             if torch.cuda.is_current_stream_capturing():
                 raise RuntimeError("run a step before capturing one")
             self._workspace = binding.adamw_workspace(device)
             self._result = torch.zeros(2, dtype=torch.float32, device=device)
+            self._norm, self._factor = self._result[0], self._result[1]
         factor = None
         if self.max_norm is not None:
-            every = tables[0] if len(tables) == 1 else binding.AdamwList([g for _, lists in parts for g in lists[0]])
+            every = parts[0][2] if len(parts) == 1 else binding.AdamwList([g for _, grads, _ in parts for g in grads])
             binding.dg_grad_norm(every, self.max_norm, self._workspace, self._result)
-            self.grad_norm, factor = self._result[0], self._result[1]
-        for (group, _), table in zip(parts, tables):
+            self.grad_norm, factor = self._norm, self._factor
+        for group, _, table in parts:
             beta1, beta2 = group["betas"]
             binding.dg_adamw_step(table, group["lr"], beta1, beta2, group["eps"], group["weight_decay"], self._workspace,
                                   factor, group["seed"])
+            table.forget_gradients()
