@@ -47,6 +47,7 @@ static void free_owned(Graph* g) {
   pool_retire(g->device, g->owned, g->owned_bytes);
   pool_retire(g->device, g->plan_memory, g->plan_bytes);
   pool_retire(g->device, g->batch_memory, g->batch_bytes);
+  free(g->batch_lengths);
   pinned_counters_retire(g->device, g->host);
   if (g->col_totals_ready) cudaEventDestroy(g->col_totals_ready);
   for (size_t i = 0; i < g->aux_event_count; ++i) cudaEventDestroy(g->aux_events[i]);
@@ -483,14 +484,36 @@ dg_status_t dg_graph_set_batch(dg_graph_t g, int64_t count, const int64_t* offse
   for (int64_t b = 0; b < count; ++b) pieces += (offsets[b + 1] - offsets[b] + rows - 1) / rows;
   const size_t offset_bytes = align256((size_t)(count + 1) * sizeof(int64_t));
   const size_t first_bytes = align256((size_t)(count + 1) * sizeof(int32_t));
-  const size_t bytes = offset_bytes + first_bytes + align256((size_t)pieces * sizeof(Piece));
+  const size_t order_bytes = align256((size_t)count * sizeof(int32_t));
+  const size_t bytes = offset_bytes + first_bytes + order_bytes + align256((size_t)pieces * sizeof(Piece));
   char* memory = nullptr;
+  int32_t* lengths = nullptr;
   if (count > 0) {
     char* host = static_cast<char*>(malloc(bytes));
-    if (!host) return invalid("out of host memory");
+    lengths = static_cast<int32_t*>(malloc((size_t)count * sizeof(int32_t)));
+    uint64_t* keys = static_cast<uint64_t*>(malloc((size_t)count * sizeof(uint64_t)));
+    if (!host || !lengths || !keys) {
+      free(host);
+      free(lengths);
+      free(keys);
+      return invalid("out of host memory");
+    }
+    // longest first, equal ones by their number
+    for (int64_t b = 0; b < count; ++b)
+      keys[b] = (uint64_t)(0xffffffffu - (uint32_t)(offsets[b + 1] - offsets[b])) << 32 | (uint32_t)b;
+    qsort(keys, (size_t)count, sizeof(uint64_t), [](const void* x, const void* y) {
+      const uint64_t p = *static_cast<const uint64_t*>(x), q = *static_cast<const uint64_t*>(y);
+      return p < q ? -1 : p > q ? 1 : 0;
+    });
+    int32_t* order = reinterpret_cast<int32_t*>(host + offset_bytes + first_bytes);
+    for (int64_t b = 0; b < count; ++b) {
+      order[b] = (int32_t)(uint32_t)keys[b];
+      lengths[b] = (int32_t)(0xffffffffu - (uint32_t)(keys[b] >> 32));
+    }
+    free(keys);
     memcpy(host, offsets, (size_t)(count + 1) * sizeof(int64_t));
     int32_t* first = reinterpret_cast<int32_t*>(host + offset_bytes);
-    Piece* piece = reinterpret_cast<Piece*>(host + offset_bytes + first_bytes);
+    Piece* piece = reinterpret_cast<Piece*>(host + offset_bytes + first_bytes + order_bytes);
     int32_t made = 0;
     for (int64_t b = 0; b < count; ++b) {
       first[b] = made;
@@ -508,6 +531,7 @@ dg_status_t dg_graph_set_batch(dg_graph_t g, int64_t count, const int64_t* offse
     free(host);
     if (e != cudaSuccess) {
       pool_retire(g->device, block, bytes);
+      free(lengths);
       return cuda_fail(e, "dg_graph_set_batch");
     }
     memory = static_cast<char*>(block);
@@ -517,7 +541,10 @@ dg_status_t dg_graph_set_batch(dg_graph_t g, int64_t count, const int64_t* offse
   g->batch_bytes = memory ? bytes : 0;
   g->batch_offsets = reinterpret_cast<const int64_t*>(memory);
   g->batch_first = memory ? reinterpret_cast<const int32_t*>(memory + offset_bytes) : nullptr;
-  g->batch_pieces = memory ? reinterpret_cast<const Piece*>(memory + offset_bytes + first_bytes) : nullptr;
+  g->batch_order = memory ? reinterpret_cast<const int32_t*>(memory + offset_bytes + first_bytes) : nullptr;
+  g->batch_pieces = memory ? reinterpret_cast<const Piece*>(memory + offset_bytes + first_bytes + order_bytes) : nullptr;
+  free(g->batch_lengths);
+  g->batch_lengths = lengths;
   g->batch_piece_count = (int32_t)pieces;
   g->batch_count = count > 0 ? count : 1;
   g->batch_rows = count > 0 ? offsets[count] : -1;

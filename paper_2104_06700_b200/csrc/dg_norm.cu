@@ -23,15 +23,83 @@ __device__ __forceinline__ void join(float& n, Moments& a, float nb, Moments b) 
   n = total;
 }
 
-// partial[piece][unit]: the moments of a channel, or, with SHARED, of a vector of channels of one group.
+// Adds `rows` of kStatRows rows (the rest are zeros) to a thread's moments: of a channel, or, with SHARED, of a vector of
+// channels of one group.  n: cells so far.
+template <int VEC, bool SHARED>
+constexpr int kUnits = SHARED ? 1 : VEC;
+template <int VEC, bool SHARED>
+__device__ __forceinline__ void add_rows(const Channels<VEC> (&v)[kStatRows], int rows, float& n, Moments (&m)[kUnits<VEC, SHARED>]) {
+  const float cells = (float)(SHARED ? rows * VEC : rows), inverse = 1.f / cells;
+  const float total = n + cells, share = cells / total;
+#pragma unroll
+  for (int k = 0; k < kUnits<VEC, SHARED>; ++k) {
+    float sum = 0.f;
+#pragma unroll
+    for (int u = 0; u < kStatRows; ++u) {
+      if constexpr (SHARED) {
+#pragma unroll
+        for (int c = 0; c < VEC; ++c) sum += v[u].v[c];
+      } else {
+        sum += v[u].v[k];
+      }
+    }
+    const float mean = sum * inverse;
+    float m2 = 0.f;
+#pragma unroll
+    for (int u = 0; u < kStatRows; ++u) {
+      if (u < rows) {
+        if constexpr (SHARED) {
+#pragma unroll
+          for (int c = 0; c < VEC; ++c) m2 = fmaf(v[u].v[c] - mean, v[u].v[c] - mean, m2);
+        } else {
+          m2 = fmaf(v[u].v[k] - mean, v[u].v[k] - mean, m2);
+        }
+      }
+    }
+    const float d = mean - m[k].mean;
+    m[k].mean = fmaf(d, share, m[k].mean);
+    m[k].m2 += m2 + d * d * (n * share);
+  }
+  n = total;
+}
+
+// Joins the moments of a block's rows in pairs, always in the same order: those of all rows are in the first `across`
+// threads, and in parts[unit * kNormThreads + thread] of them.
+template <int UNITS>
+__device__ __forceinline__ void join_block(float& n, Moments (&m)[UNITS], Moments* parts, float* counts, int32_t across, int32_t down) {
+  counts[threadIdx.x] = n;
+#pragma unroll
+  for (int k = 0; k < UNITS; ++k) parts[k * kNormThreads + threadIdx.x] = m[k];
+  const int32_t y = threadIdx.x / across;
+  int half = 1;
+  while (half < down) half *= 2;
+  for (half /= 2; half > 0; half /= 2) {
+    __syncthreads();
+    const int other = threadIdx.x + half * across;
+    if (y < half && y + half < down) {
+      const float nb = counts[other];
+      float total = n;
+#pragma unroll
+      for (int k = 0; k < UNITS; ++k) {
+        total = n;
+        join(total, m[k], nb, parts[k * kNormThreads + other]);
+        parts[k * kNormThreads + threadIdx.x] = m[k];
+      }
+      n = total;
+      counts[threadIdx.x] = n;
+    }
+  }
+}
+
+// partial[piece][unit]: the moments of a piece's rows.
 template <typename X, int VEC, bool SHARED>
-__global__ void __launch_bounds__(kNormThreads) norm_stats_kernel(NormArgs a, NormShape sh, const Piece* pieces, float2* partial) {
-  constexpr int kUnits = SHARED ? 1 : VEC;
-  constexpr float kCells = SHARED ? VEC : 1;
-  __shared__ Moments parts[kNormThreads * kUnits];
+__global__ void __launch_bounds__(kNormThreads, VEC == 8 ? 2 : 4)
+    norm_stats_kernel(NormArgs a, NormShape sh, const Piece* pieces, float2* partial) {
+  constexpr int kEach = kUnits<VEC, SHARED>;
+  __shared__ Moments parts[kNormThreads * kEach];
   __shared__ float counts[kNormThreads];
   const Place at = place_of(a, sh, pieces, blockIdx.x);
-  Moments m[kUnits] = {};
+  Moments m[kEach] = {};
   float n = 0.f;
   if (at.channel < a.F) {
     const X* x = static_cast<const X*>(a.X) + (int64_t)at.piece.row * a.F + at.channel;
@@ -41,116 +109,179 @@ __global__ void __launch_bounds__(kNormThreads) norm_stats_kernel(NormArgs a, No
 #pragma unroll
       for (int u = 0; u < kStatRows; ++u) {
         const int32_t r = r0 + u * at.down;
+        v[u] = Channels<VEC>{};
         if (r < at.piece.rows) {
           v[u] = load_channels<X, VEC>(x + (int64_t)r * a.F);
           ++rows;
-        } else {
-#pragma unroll
-          for (int c = 0; c < VEC; ++c) v[u].v[c] = 0.f;
         }
       }
-      const float cells = rows * kCells, inverse = 1.f / cells;
-      const float total = n + cells, share = cells / total;
-#pragma unroll
-      for (int k = 0; k < kUnits; ++k) {
-        float sum = 0.f;
-#pragma unroll
-        for (int u = 0; u < kStatRows; ++u) {
-          if constexpr (SHARED) {
-#pragma unroll
-            for (int c = 0; c < VEC; ++c) sum += v[u].v[c];
-          } else {
-            sum += v[u].v[k];
-          }
-        }
-        const float mean = sum * inverse;
-        float m2 = 0.f;
-#pragma unroll
-        for (int u = 0; u < kStatRows; ++u) {
-          if (u < rows) {
-            if constexpr (SHARED) {
-#pragma unroll
-              for (int c = 0; c < VEC; ++c) m2 = fmaf(v[u].v[c] - mean, v[u].v[c] - mean, m2);
-            } else {
-              m2 = fmaf(v[u].v[k] - mean, v[u].v[k] - mean, m2);
-            }
-          }
-        }
-        const float d = mean - m[k].mean;
-        m[k].mean = fmaf(d, share, m[k].mean);
-        m[k].m2 += m2 + d * d * (n * share);
-      }
-      n = total;
+      add_rows<VEC, SHARED>(v, rows, n, m);
     }
   }
-  counts[threadIdx.x] = n;
-#pragma unroll
-  for (int k = 0; k < kUnits; ++k) parts[k * kNormThreads + threadIdx.x] = m[k];
-  // the rows' threads in pairs, always in the same order
-  int half = 1;
-  while (half < sh.down) half *= 2;
-  for (half /= 2; half > 0; half /= 2) {
-    __syncthreads();
-    const int other = threadIdx.x + half * sh.across;
-    if (at.y < half && at.y + half < sh.down) {
-      const float nb = counts[other];
-      float total = n;
-#pragma unroll
-      for (int k = 0; k < kUnits; ++k) {
-        total = n;
-        join(total, m[k], nb, parts[k * kNormThreads + other]);
-        parts[k * kNormThreads + threadIdx.x] = m[k];
-      }
-      n = total;
-      counts[threadIdx.x] = n;
-    }
-  }
+  join_block<kEach>(n, m, parts, counts, sh.across, sh.down);
   if (at.y == 0 && at.channel < a.F) {
-    const int32_t units = a.F / VEC * kUnits;
-    float2* out = partial + (int64_t)blockIdx.x * units + at.channel / VEC * kUnits;
+    const int32_t units = a.F / VEC * kEach;
+    float2* out = partial + (int64_t)blockIdx.x * units + at.channel / VEC * kEach;
 #pragma unroll
-    for (int k = 0; k < kUnits; ++k) out[k] = make_float2(m[k].mean, m[k].m2);
+    for (int k = 0; k < kEach; ++k) out[k] = make_float2(m[k].mean, m[k].m2);
   }
 }
 
-// stats of a group from its pieces' moments, in 64 bits; `units` moments of `cells` channels each for a group.
-__global__ void __launch_bounds__(kNormThreads) norm_join_kernel(NormArgs a, NormShape sh, const Piece* pieces, const int32_t* first,
-                                                                  const float2* partial, int32_t units, int32_t cells) {
+// Short graphs: statistics and results in one launch.
+template <typename X, typename Y, int ACT, int VEC, bool SHARED>
+__global__ void __launch_bounds__(kNormThreads, VEC == 8 ? 2 : 3) norm_graph_kernel(NormArgs a, GraphShape sh) {
+  constexpr int kEach = kUnits<VEC, SHARED>;
+  __shared__ Moments parts[kNormThreads * kEach];
+  __shared__ float counts[kNormThreads];
+  __shared__ float2 group_parts[kTileGroups], group_stats[kTileGroups];
+  graph_kernel_begins();
+  const GraphPlace at = graph_place(a, sh);
+  const int32_t rows = (int32_t)(at.rows.hi - at.rows.lo);
+  const int32_t chunk = at.step * kStatRows, chunks = (rows + chunk - 1) / chunk;
+  const int64_t base = at.rows.lo * a.F + at.channel;
+  const X* x = static_cast<const X*>(a.X) + base;
+  Y* y = static_cast<Y*>(a.out) + base;
+  const bool mine = at.channel < a.F;
+  RawChannels<X, VEC> raw[kStatRows];
+  auto load = [&](int32_t r0) {
+#pragma unroll
+    for (int u = 0; u < kStatRows; ++u) {
+      raw[u] = RawChannels<X, VEC>{};
+      if (r0 + u * at.step < rows) raw[u] = load_raw<X, VEC>(x + (int64_t)(r0 + u * at.step) * a.F);
+    }
+  };
+  Moments m[kEach] = {};
+  float n = 0.f;
+  if (mine) {
+    for (int32_t c = 0; c < chunks; ++c) {
+      const int32_t r0 = c * chunk + at.y;
+      load(r0);
+      if (r0 >= rows) break;  // of the last chunk: it stays in `raw` for what follows, as nothing
+      Channels<VEC> v[kStatRows];
+      int count = 0;
+#pragma unroll
+      for (int u = 0; u < kStatRows; ++u) {
+        v[u] = numbers_of(raw[u]);
+        count += r0 + u * at.step < rows;
+      }
+      add_rows<VEC, SHARED>(v, count, n, m);
+    }
+  }
+  join_block<kEach>(n, m, parts, counts, sh.across, sh.down);
+  __syncthreads();
+  // a warp for a group: its units have the same count each
+  const int lane = threadIdx.x & 31, warp = threadIdx.x / 32;
+  const int32_t groups = at.tile_channels / a.width, units = SHARED ? a.width / VEC : a.width;
+  const float count = (float)rows_of_rank(at, sh, at.rank) * (SHARED ? VEC : 1);
+  auto unit = [&](int32_t g, int32_t k) {
+    const int32_t u = g * units + k;
+    return SHARED ? parts[u] : parts[u % VEC * kNormThreads + u / VEC];
+  };
+  for (int32_t g = warp; g < groups; g += kNormThreads / 32) {
+    float sum = 0.f;
+    for (int32_t k = lane; k < units; k += 32) sum += unit(g, k).mean;
+    const float mean = warp_total(sum) / units;
+    sum = 0.f;
+    for (int32_t k = lane; k < units; k += 32) {
+      const Moments u = unit(g, k);
+      sum += fmaf(count * (u.mean - mean), u.mean - mean, u.m2);
+    }
+    sum = warp_total(sum);
+    if (lane == 0) group_parts[g] = make_float2(mean, sum);
+  }
+  if (sh.cluster > 1) {
+    cluster_arrive();
+    cluster_wait();
+  }
+  __syncthreads();
+  const float cells = rows > 0 ? (float)rows * a.width : 1.f;
+  for (int32_t g = threadIdx.x; g < groups; g += kNormThreads) {
+    float2 p = group_parts[g];
+    if (sh.cluster > 1) {
+      // the blocks' parts, in the order of their ranks
+      float part_cells = 0.f;
+      Moments all = {0.f, 0.f};
+      for (int32_t r = 0; r < sh.cluster; ++r) {
+        const float2 o = of_rank(group_parts + g, r);
+        join(part_cells, all, (float)rows_of_rank(at, sh, r) * a.width, Moments{o.x, o.y});
+      }
+      p = make_float2(all.mean, all.m2);
+    }
+    const float2 st = make_float2(p.x, 1.f / sqrtf(p.y / cells + a.eps));
+    group_stats[g] = st;
+    if (at.rank == 0) a.stats[(int64_t)at.graph * a.groups + at.tile_first / a.width + g] = st;
+  }
+  if (sh.cluster > 1) cluster_arrive();  // the others' shared memory has been read
+  __syncthreads();
+  if (mine) {
+    float mean[VEC], rstd[VEC], w[VEC], b[VEC];
+#pragma unroll
+    for (int c = 0; c < VEC; ++c) {
+      const float2 st = group_stats[(at.channel - at.tile_first + c) / a.width];
+      mean[c] = st.x, rstd[c] = st.y;
+      w[c] = a.weight ? a.weight[at.channel + c] : 1.f;
+      b[c] = a.bias ? a.bias[at.channel + c] : 0.f;
+    }
+    for (int32_t c = chunks - 1; c >= 0; --c) {
+      const int32_t r0 = c * chunk + at.y;
+      if (c < chunks - 1) load(r0);
+#pragma unroll
+      for (int u = 0; u < kStatRows; ++u) {
+        if (r0 + u * at.step >= rows) break;
+        Channels<VEC> v = numbers_of(raw[u]);
+#pragma unroll
+        for (int k = 0; k < VEC; ++k) v.v[k] = activated<ACT>(fmaf((v.v[k] - mean[k]) * rstd[k], w[k], b[k]));
+        store_channels<Y, VEC>(y + (int64_t)(r0 + u * at.step) * a.F, v);
+      }
+    }
+  }
+  if (sh.cluster > 1) cluster_wait();
+  graph_kernel_ends();
+}
+
+// stats of a group from its pieces' moments, in 64 bits; `units` moments of `cells` channels each for a group.  A block, or
+// with PER_WARP a warp, for a group: `lanes` threads (a power of two) along the units, the others along the
+// pieces.  Means are taken from the first one on, so that one pass is enough: the differences' squares are exact.
+template <bool PER_WARP>
+__global__ void norm_join_kernel(NormArgs a, NormShape sh, const Piece* pieces, const int32_t* first, const float2* partial,
+                                 int32_t units, int32_t cells, int32_t lanes) {
   cudaGridDependencySynchronize();
-  const int64_t graph = blockIdx.x / a.groups;
-  const int32_t group = (int32_t)(blockIdx.x % a.groups);
+  const int32_t thread = PER_WARP ? threadIdx.x & 31 : threadIdx.x;
+  const int64_t pair = PER_WARP ? (int64_t)blockIdx.x * (blockDim.x / 32) + threadIdx.x / 32 : blockIdx.x;
+  if (pair >= a.graphs * a.groups) return;
+  const int64_t graph = pair / a.groups;
+  const int32_t group = (int32_t)(pair % a.groups);
   const Rows r = rows_of(a, graph);
   const int32_t lo = first ? first[graph] : 0, hi = first ? first[graph + 1] : sh.pieces;
-  const int64_t entries = (int64_t)(hi - lo) * units;
   const double n = r.hi > r.lo ? (double)(r.hi - r.lo) * a.width : 1.0;
-  auto rows = [&](int32_t p) {
-    if (pieces) return pieces[p].rows;
-    const int64_t left = a.rows - (int64_t)p * sh.rows;
-    return (int32_t)(left < sh.rows ? left : sh.rows);
-  };
-  auto moments = [&](int64_t e, double* count) {
-    const int32_t p = lo + (int32_t)(e / units);
-    *count = (double)rows(p) * cells;
-    return partial[((int64_t)p * a.groups + group) * units + e % units];
-  };
-  double sum = 0.0, count;
-  for (int64_t e = threadIdx.x; e < entries; e += blockDim.x) {
-    const float2 m = moments(e, &count);
-    sum += count * m.x;
+  const float2* mine = partial + (int64_t)group * units;
+  const int64_t stride = (int64_t)a.groups * units;
+  const int32_t down = (PER_WARP ? 32 : blockDim.x) / lanes;
+  const double from = hi > lo ? mine[lo * stride].x : 0.f;
+  double sum = 0.0, squares = 0.0;
+#pragma unroll 4
+  for (int32_t p = lo + thread / lanes; p < hi; p += down) {
+    const double rows = pieces ? pieces[p].rows : p + 1 < sh.pieces ? sh.rows : (int32_t)(a.rows - (int64_t)p * sh.rows);
+    double s1 = 0.0, s2 = 0.0;
+    for (int32_t k = thread % lanes; k < units; k += lanes) {
+      const float2 m = mine[p * stride + k];
+      const double d = m.x - from;
+      s1 += d;
+      s2 += m.y + rows * cells * d * d;
+    }
+    sum += rows * cells * s1;
+    squares += s2;
   }
-  const double mean = block_sum(sum) / n;
-  sum = 0.0;
-  for (int64_t e = threadIdx.x; e < entries; e += blockDim.x) {
-    const float2 m = moments(e, &count);
-    const double d = m.x - mean;
-    sum += m.y + count * d * d;
-  }
-  sum = block_sum(sum);
-  if (threadIdx.x == 0) a.stats[blockIdx.x] = make_float2((float)mean, (float)(1.0 / sqrt(sum / n + (double)a.eps)));
+  sum = PER_WARP ? warp_sum(sum) : block_sum(sum);
+  squares = PER_WARP ? warp_sum(squares) : block_sum(squares);
+  const double off = sum / n, var = squares / n - off * off;
+  // from and the moments of no rows are 0; a variance below 0 is one of rounding (NaN stays NaN)
+  if (thread == 0)
+    a.stats[pair] = make_float2((float)(from + off), (float)(1.0 / sqrt((var < 0.0 ? 0.0 : var) + (double)a.eps)));
 }
 
 template <typename X, typename Y, int ACT, int VEC>
-__global__ void __launch_bounds__(kNormThreads) norm_apply_kernel(NormArgs a, NormShape sh, const Piece* pieces) {
+__global__ void __launch_bounds__(kNormThreads, VEC == 8 ? 2 : 4) norm_apply_kernel(NormArgs a, NormShape sh, const Piece* pieces) {
   constexpr int kRows = 4;
   cudaGridDependencySynchronize();
   const Place at = place_of(a, sh, pieces, gridDim.x - 1 - blockIdx.x);
@@ -209,8 +340,17 @@ __global__ void __launch_bounds__(kNormThreads) norm_fwd_direct_kernel(NormArgs 
 template <typename X, typename Y, int ACT>
 dg_status_t forward(const Graph* g, const NormArgs& a, dg_type_t x, dg_type_t y, cudaStream_t s) {
   const int vec = norm_vector(a, x, y);
-  const NormShape sh = norm_shape(g, a, vec);
   const bool shared = vec > 1 && a.width % vec == 0;
+  if (const GraphPlan plan = graph_plan(g, a, vec, sizeof(X), kStatRows); plan.graphs > 0) {
+    DG_CUDA((by_vector<sizeof(X) == 2 && sizeof(Y) == 2>(vec, [&](auto v) {
+      constexpr int VEC = decltype(v)::value;
+      return shared ? launch_graphs(plan, norm_graph_kernel<X, Y, ACT, VEC, true>, s, a)
+                    : launch_graphs(plan, norm_graph_kernel<X, Y, ACT, VEC, false>, s, a);
+    })));
+    count_launches((plan.long_graphs > 0) + (plan.graphs > plan.long_graphs));
+    return DG_OK;
+  }
+  const NormShape sh = norm_shape(g, a, vec);
   const int32_t units = shared ? a.F / vec : a.F;
   void* memory = nullptr;
   if (sh.pieces > 0 && scratch_alloc(g, (size_t)sh.pieces * units * sizeof(float2), s, &memory) != cudaSuccess) {
@@ -234,10 +374,16 @@ dg_status_t forward(const Graph* g, const NormArgs& a, dg_type_t x, dg_type_t y,
     });
   cudaError_t e = cudaGetLastError();
   // a warp joins a few pieces, a block many
-  const int threads = sh.pieces / a.graphs * (units / a.groups) > 64 ? kNormThreads : 32;
+  const int32_t of_group = units / a.groups;
+  int32_t lanes = 1;
+  while (lanes < of_group && lanes < 32) lanes *= 2;
+  const int32_t cells = shared ? vec : 1;
+  const int64_t pairs = a.graphs * a.groups;
   if (e == cudaSuccess)
-    e = launch_kernel(norm_join_kernel, dim3((unsigned)(a.graphs * a.groups)), threads, s, true, a, sh, pieces, g->batch_first,
-                      (const float2*)partial, units / a.groups, shared ? (int32_t)vec : (int32_t)1);
+    e = pieces ? launch_kernel(norm_join_kernel<true>, dim3((unsigned)((pairs + 7) / 8)), kNormThreads, s, true, a, sh, pieces,
+                               g->batch_first, (const float2*)partial, of_group, cells, lanes)
+               : launch_kernel(norm_join_kernel<false>, dim3((unsigned)pairs), 512, s, true, a, sh, pieces, g->batch_first,
+                               (const float2*)partial, of_group, cells, lanes);
   if (e == cudaSuccess && sh.pieces > 0)
     e = by_vector<sizeof(X) == 2 && sizeof(Y) == 2>(vec, [&](auto v) {
       return launch_kernel(norm_apply_kernel<X, Y, ACT, decltype(v)::value>, grid, kNormThreads, s, true, a, sh, pieces);
@@ -256,6 +402,46 @@ int norm_vector(const NormArgs& a, dg_type_t x, dg_type_t y) {
   // forward: Y has the type y; backward: dX has the type x
   while (vec > 1 && !(a.F % vec == 0 && fits(a.X, x) && fits(a.dY, y) && fits(a.out, a.dY ? x : y))) vec /= 2;
   return vec;
+}
+
+GraphPlan graph_plan(const Graph* g, const NormArgs& a, int vec, int x_bytes, int rows_kept) {
+  GraphPlan plan{};
+  GraphShape& sh = plan.shape;
+  const int64_t longest = g->batch_longest < 0 ? g->n : g->batch_longest;
+  const int32_t vectors = a.F / vec;
+  // the fewest vectors that whole groups fill
+  int32_t least = a.width;
+  while (least % vec) least += a.width;
+  least /= vec;
+  if (least > kNormThreads) return plan;
+  // lines of 128 bytes, or sectors of 32 where the graphs are few
+  auto tile = [&](int bytes) {
+    int32_t across = least;
+    while (across * vec * x_bytes < bytes && across + least <= vectors && across + least <= kNormThreads) across += least;
+    return across;
+  };
+  sh.across = tile(128);
+  if (a.graphs * (vectors / sh.across) < g->sm_count) sh.across = tile(32);
+  sh.vec = vec;
+  sh.down = kNormThreads / sh.across;
+  sh.tiles = (vectors + sh.across - 1) / sh.across;
+  sh.order = g->batch_order;
+  const int64_t kept = (int64_t)sh.down * rows_kept;  // rows in a block's registers
+  if (longest > 4 * kCluster * kept) return plan;
+  if (a.graphs * sh.tiles * kCluster >= ((int64_t)1 << 31)) return plan;
+  plan.graphs = a.graphs;
+  if (!g->batch_lengths) {
+    plan.long_graphs = 1;
+  } else {
+    // graphs, longest first, of more than two registerfuls of a block
+    int64_t lo = 0, hi = a.graphs;
+    while (lo < hi) {
+      const int64_t mid = (lo + hi) / 2;
+      if (g->batch_lengths[mid] > 2 * kept) lo = mid + 1; else hi = mid;
+    }
+    plan.long_graphs = lo;
+  }
+  return plan;
 }
 
 NormShape norm_shape(const Graph* g, const NormArgs& a, int vec) {
@@ -278,7 +464,8 @@ NormShape norm_shape(const Graph* g, const NormArgs& a, int vec) {
     sh.pieces = g->batch_piece_count;
     return sh;
   }
-  const int64_t blocks = (int64_t)g->sm_count * 6 / sh.tiles;
+  // one wave of the kernels that keep four blocks on an SM, two of those that keep two
+  const int64_t blocks = (int64_t)g->sm_count * 4 / sh.tiles;
   int64_t rows = (a.rows + blocks - 1) / (blocks > 0 ? blocks : 1);
   const int64_t least = (int64_t)sh.down * 8;
   if (rows < least) rows = least;

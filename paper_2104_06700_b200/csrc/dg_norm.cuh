@@ -153,6 +153,56 @@ __device__ __forceinline__ void store_channels(T* p, const Channels<VEC>& r) {
   }
 }
 
+// The same as it is stored: what waits in registers for the second use.
+template <typename T, int VEC>
+struct RawChannels {
+  std::conditional_t<sizeof(T) * VEC == 16, uint4,
+                     std::conditional_t<sizeof(T) * VEC == 8, uint2, std::conditional_t<sizeof(T) * VEC == 4, uint32_t, uint16_t>>> v;
+};
+template <typename T, int VEC>
+__device__ __forceinline__ RawChannels<T, VEC> load_raw(const T* p) {
+  RawChannels<T, VEC> r;
+  r.v = *reinterpret_cast<const decltype(r.v)*>(p);
+  return r;
+}
+template <typename T, int VEC>
+__device__ __forceinline__ Channels<VEC> numbers_of(const RawChannels<T, VEC>& q) {
+  uint32_t w[4] = {};
+  if constexpr (sizeof(T) * VEC == 16)
+    w[0] = q.v.x, w[1] = q.v.y, w[2] = q.v.z, w[3] = q.v.w;
+  else if constexpr (sizeof(T) * VEC == 8)
+    w[0] = q.v.x, w[1] = q.v.y;
+  else
+    w[0] = q.v;
+  Channels<VEC> r;
+#pragma unroll
+  for (int c = 0; c < VEC; ++c) {
+    if constexpr (sizeof(T) == 4)
+      r.v[c] = __uint_as_float(w[c]);
+    else
+      r.v[c] = __uint_as_float(c % 2 ? w[c / 2] & 0xffff0000u : w[c / 2] << 16);
+  }
+  return r;
+}
+
+// A thread's channels: what does not change along its rows.
+template <int VEC>
+struct Fixed {
+  float mean[VEC], rstd[VEC], w[VEC], b[VEC];
+};
+template <int VEC>
+__device__ __forceinline__ Fixed<VEC> fixed_of(const NormArgs& a, int32_t graph, int32_t channel) {
+  Fixed<VEC> f;
+#pragma unroll
+  for (int c = 0; c < VEC; ++c) {
+    const float2 st = a.stats[(int64_t)graph * a.groups + (channel + c) / a.width];
+    f.mean[c] = st.x, f.rstd[c] = st.y;
+    f.w[c] = a.weight ? a.weight[channel + c] : 1.f;
+    f.b[c] = a.bias ? a.bias[channel + c] : 0.f;
+  }
+  return f;
+}
+
 // Where a thread works: its piece, its first channel, its place along the rows.
 struct Place {
   Piece piece;
@@ -200,18 +250,119 @@ auto by_vector(int vec, Fn f) {
   return f(std::integral_constant<int, 1>());
 }
 
+__device__ __forceinline__ double warp_sum(double v) {
+#pragma unroll
+  for (int o = 16; o > 0; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
+  return v;
+}
 // The sum of v over a block of at most 1024 threads, in every thread and always in the same order.
 __device__ __forceinline__ double block_sum(double v) {
   __shared__ double sums[32];
-#pragma unroll
-  for (int o = 16; o > 0; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
-  if (blockDim.x == 32) return v;
+  v = warp_sum(v);
   __syncthreads();  // the last call's sums have been read
   if (threadIdx.x % 32 == 0) sums[threadIdx.x / 32] = v;
   __syncthreads();
   v = 0.0;
   for (int i = 0; i < (int)blockDim.x / 32; ++i) v += sums[i];
   return v;
+}
+
+// ---- a cluster of blocks for a graph and a tile of channels: short graphs -------------------------------------------
+
+// A cluster of blocks takes the rows of one graph in the channels of a tile, which holds whole groups: what it sums it
+// needs nowhere else, and rows that fit its registers are read once.
+constexpr int kCluster = 8;
+constexpr int kTileGroups = 128;  // most groups of a tile
+struct GraphShape {
+  int32_t vec, across, down, tiles;
+  int32_t cluster;       // blocks: 1 or kCluster
+  int32_t first;         // place in `order` of the launch's first graph
+  const int32_t* order;  // graphs, longest first; null: one graph
+};
+// A call's two launches: long graphs, then the others.
+struct GraphPlan {
+  GraphShape shape;
+  int64_t long_graphs, graphs;  // 0 graphs: not a call for these kernels
+};
+GraphPlan graph_plan(const Graph* g, const NormArgs& a, int vec, int x_bytes, int rows_kept);
+
+struct GraphPlace {
+  int32_t graph, rank, cluster;
+  int32_t channel, tile_channels;  // the thread's first channel (>= F: none), those of the tile
+  int32_t tile_first;
+  int32_t y, step;                 // its first row of the graph, and the distance to its next
+  Rows rows;
+};
+__device__ __forceinline__ GraphPlace graph_place(const NormArgs& a, const GraphShape& sh) {
+  GraphPlace r;
+  r.cluster = sh.cluster;
+  const int64_t item = blockIdx.x / sh.cluster;
+  r.rank = (int32_t)(blockIdx.x % sh.cluster);
+  const int32_t at = sh.first + (int32_t)(item / sh.tiles), tile = (int32_t)(item % sh.tiles);
+  r.graph = sh.order ? sh.order[at] : 0;
+  r.rows = rows_of(a, r.graph);
+  r.tile_first = tile * sh.across * sh.vec;
+  r.tile_channels = min(sh.across * sh.vec, a.F - r.tile_first);
+  const int32_t y = threadIdx.x / sh.across, x = threadIdx.x % sh.across * sh.vec;
+  r.channel = y < sh.down && x < r.tile_channels ? r.tile_first + x : a.F;
+  r.y = r.rank * sh.down + y;
+  r.step = sh.cluster * sh.down;
+  return r;
+}
+// Rows that a block of the cluster has.
+__device__ __forceinline__ int32_t rows_of_rank(const GraphPlace& at, const GraphShape& sh, int32_t rank) {
+  const int32_t rows = (int32_t)(at.rows.hi - at.rows.lo), rest = rows % at.step - rank * sh.down;
+  return rows / at.step * sh.down + min(max(rest, 0), sh.down);
+}
+__device__ __forceinline__ void cluster_arrive() { asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory"); }
+__device__ __forceinline__ void cluster_wait() { asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory"); }
+// The pair of numbers at the same place in another block's shared memory.
+__device__ __forceinline__ float2 of_rank(const float2* p, int32_t rank) {
+  const uint32_t mine = (uint32_t)__cvta_generic_to_shared(p);
+  uint32_t there;
+  asm("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(there) : "r"(mine), "r"(rank));
+  float2 r;
+  asm volatile("ld.shared::cluster.v2.f32 {%0, %1}, [%2];" : "=f"(r.x), "=f"(r.y) : "r"(there));
+  return r;
+}
+__device__ __forceinline__ float warp_total(float v) {
+#pragma unroll
+  for (int o = 16; o > 0; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
+  return v;
+}
+// The launch of the other graphs may begin once all blocks of this one have; it ends behind it, by its last block.
+__device__ __forceinline__ void graph_kernel_begins() { cudaTriggerProgrammaticLaunchCompletion(); }
+__device__ __forceinline__ void graph_kernel_ends() {
+  if (blockIdx.x == gridDim.x - 1) cudaGridDependencySynchronize();
+}
+
+// Both launches of a plan.
+template <typename... P, typename... A>
+cudaError_t launch_graphs(const GraphPlan& plan, void (*kernel)(NormArgs, GraphShape, P...), cudaStream_t s, const NormArgs& a,
+                          const A&... args) {
+  const int64_t counts[2] = {plan.long_graphs, plan.graphs - plan.long_graphs};
+  bool before = false;
+  for (int i = 0; i < 2; ++i) {
+    if (counts[i] == 0) continue;
+    GraphShape sh = plan.shape;
+    sh.cluster = i == 0 ? kCluster : 1;
+    sh.first = i == 0 ? 0 : (int32_t)plan.long_graphs;
+    cudaLaunchAttribute attributes[2] = {};
+    attributes[0].id = cudaLaunchAttributeClusterDimension;
+    attributes[0].val.clusterDim.x = (unsigned)sh.cluster;
+    attributes[0].val.clusterDim.y = attributes[0].val.clusterDim.z = 1;
+    attributes[1].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attributes[1].val.programmaticStreamSerializationAllowed = 1;
+    cudaLaunchConfig_t config{};
+    config.gridDim = dim3((unsigned)(counts[i] * sh.tiles * sh.cluster));
+    config.blockDim = dim3(kNormThreads);
+    config.stream = s;
+    config.attrs = attributes;
+    config.numAttrs = before ? 2 : 1;
+    if (cudaError_t e = cudaLaunchKernelEx(&config, kernel, a, sh, args...)) return e;
+    before = true;
+  }
+  return cudaSuccess;
 }
 
 // ---- one block for a group, where a call has no scratch ---------------------------------------------------------

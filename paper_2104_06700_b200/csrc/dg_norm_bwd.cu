@@ -9,24 +9,6 @@ namespace {
 
 constexpr int kRows = 4;  // in flight per thread, of each matrix
 
-// A thread's channels: what does not change along its rows.
-template <int VEC>
-struct Fixed {
-  float mean[VEC], rstd[VEC], w[VEC], b[VEC];
-};
-template <int VEC>
-__device__ __forceinline__ Fixed<VEC> fixed_of(const NormArgs& a, int32_t graph, int32_t channel) {
-  Fixed<VEC> f;
-#pragma unroll
-  for (int c = 0; c < VEC; ++c) {
-    const float2 st = a.stats[(int64_t)graph * a.groups + (channel + c) / a.width];
-    f.mean[c] = st.x, f.rstd[c] = st.y;
-    f.w[c] = a.weight ? a.weight[channel + c] : 1.f;
-    f.b[c] = a.bias ? a.bias[channel + c] : 0.f;
-  }
-  return f;
-}
-
 // partial[piece][channel] = (sum of d, sum of d hat).  The sums of every kRows rows are added to the thread's.
 template <typename X, typename Y, int ACT, int VEC>
 __global__ void __launch_bounds__(kNormThreads) norm_sums_kernel(NormArgs a, NormShape sh, const Piece* pieces, float2* partial) {
@@ -88,51 +70,236 @@ __global__ void __launch_bounds__(kNormThreads) norm_sums_kernel(NormArgs a, Nor
   }
 }
 
-// The first graphs x groups blocks: (A, B) of a group.  The others: the gradients of weight and bias of 8 channels each,
-// a warp along the pieces for a channel.  Sums in 64 bits.
-__global__ void __launch_bounds__(kNormThreads)
-    norm_join_sums_kernel(NormArgs a, NormShape sh, const int32_t* first, const float2* partial, float2* means, float* dweight,
-                          float* dbias) {
-  cudaGridDependencySynchronize();
-  const int64_t pairs = means ? a.graphs * a.groups : 0;
-  if (blockIdx.x < pairs) {
-    const int64_t graph = blockIdx.x / a.groups;
-    const int32_t group = (int32_t)(blockIdx.x % a.groups);
-    const Rows r = rows_of(a, graph);
-    const int32_t lo = first ? first[graph] : 0, hi = first ? first[graph + 1] : sh.pieces;
-    const int64_t entries = (int64_t)(hi - lo) * a.width;
-    double s1 = 0.0, s2 = 0.0;
-    for (int64_t e = threadIdx.x; e < entries; e += blockDim.x) {
-      const int32_t channel = group * a.width + (int32_t)(e % a.width);
-      const float2 p = partial[(lo + e / a.width) * a.F + channel];
-      const double w = a.weight ? a.weight[channel] : 1.f;
-      s1 += w * p.x;
-      s2 += w * p.y;
-    }
-    s1 = block_sum(s1);
-    s2 = block_sum(s2);
-    const double n = r.hi > r.lo ? (double)(r.hi - r.lo) * a.width : 1.0;
-    if (threadIdx.x == 0) means[blockIdx.x] = make_float2((float)(s1 / n), (float)(s2 / n));
-    return;
-  }
-  const int lane = threadIdx.x & 31, warps = blockDim.x / 32;
-  const int64_t c = (blockIdx.x - pairs) * warps + threadIdx.x / 32;
-  if (c >= a.F) return;
+constexpr int kJoinThreads = 512;
+
+// (A, B) of a group from its pieces' sums, in 64 bits: `lanes` threads (a power of two) along its channels, the others along
+// the pieces.
+__device__ __forceinline__ void join_means(const NormArgs& a, const NormShape& sh, const int32_t* first, const float2* partial,
+                                           float2* means, int32_t lanes, int64_t pair, int32_t thread, int32_t threads, bool warp) {
+  const int64_t graph = pair / a.groups;
+  const int32_t group = (int32_t)(pair % a.groups);
+  const Rows r = rows_of(a, graph);
+  const int32_t lo = first ? first[graph] : 0, hi = first ? first[graph + 1] : sh.pieces;
+  const int32_t down = threads / lanes;
   double s1 = 0.0, s2 = 0.0;
-  for (int32_t p = lane; p < sh.pieces; p += 32) {
-    const float2 v = partial[(int64_t)p * a.F + c];
-    s1 += v.x;
-    s2 += v.y;
+  for (int32_t k = thread % lanes; k < a.width; k += lanes) {
+    const int32_t channel = group * a.width + k;
+    const double w = a.weight ? a.weight[channel] : 1.f;
+    double t1 = 0.0, t2 = 0.0;
+#pragma unroll 4
+    for (int32_t p = lo + thread / lanes; p < hi; p += down) {
+      const float2 v = partial[(int64_t)p * a.F + channel];
+      t1 += v.x;
+      t2 += v.y;
+    }
+    s1 += w * t1;
+    s2 += w * t2;
   }
+  s1 = warp ? warp_sum(s1) : block_sum(s1);
+  s2 = warp ? warp_sum(s2) : block_sum(s2);
+  const double n = r.hi > r.lo ? (double)(r.hi - r.lo) * a.width : 1.0;
+  if (thread == 0) means[pair] = make_float2((float)(s1 / n), (float)(s2 / n));
+}
+
+// The gradients of weight and bias of 8 channels: 64 threads along the `rows` rows of sums.  In 64 bits.
+__device__ __forceinline__ void join_weights(int32_t F, const float2* partial, int64_t rows, float* dweight, float* dbias, int32_t tile) {
+  __shared__ double2 sums[kJoinThreads];
+  const int32_t c = tile * 8 + threadIdx.x % 8;
+  double s1 = 0.0, s2 = 0.0;
+  if (c < F) {
+#pragma unroll 8
+    for (int64_t p = threadIdx.x / 8; p < rows; p += kJoinThreads / 8) {
+      const float2 v = partial[p * F + c];
+      s1 += v.x;
+      s2 += v.y;
+    }
+  }
+  sums[threadIdx.x] = make_double2(s1, s2);
+  for (int half = kJoinThreads / 2; half >= 8; half /= 2) {
+    __syncthreads();
+    if (threadIdx.x < half) {
+      sums[threadIdx.x].x += sums[threadIdx.x + half].x;
+      sums[threadIdx.x].y += sums[threadIdx.x + half].y;
+    }
+  }
+  if (threadIdx.x >= 8 || c >= F) return;
+  if (dbias) dbias[c] = (float)sums[threadIdx.x].x;
+  if (dweight) dweight[c] = (float)sums[threadIdx.x].y;
+}
+
+// One graph: a block for a group, then the blocks of the weights.
+__global__ void __launch_bounds__(kJoinThreads)
+    norm_join_sums_kernel(NormArgs a, NormShape sh, const float2* partial, float2* means, float* dweight, float* dbias, int32_t lanes) {
+  cudaGridDependencySynchronize();
+  const int32_t pairs = means ? a.groups : 0;
+  if (blockIdx.x < pairs)
+    join_means(a, sh, nullptr, partial, means, lanes, blockIdx.x, threadIdx.x, kJoinThreads, false);
+  else
+    join_weights(a.F, partial, sh.pieces, dweight, dbias, blockIdx.x - pairs);
+}
+// Many graphs: a warp for a group.
+__global__ void __launch_bounds__(kNormThreads)
+    norm_join_means_kernel(NormArgs a, NormShape sh, const int32_t* first, const float2* partial, float2* means, int32_t lanes) {
+  cudaGridDependencySynchronize();
+  const int64_t pair = (int64_t)blockIdx.x * (kNormThreads / 32) + threadIdx.x / 32;
+  if (pair < a.graphs * a.groups) join_means(a, sh, first, partial, means, lanes, pair, threadIdx.x % 32, 32, true);
+}
+__global__ void __launch_bounds__(kJoinThreads)
+    norm_weight_sums_kernel(int32_t F, const float2* partial, int64_t rows, float* dweight, float* dbias) {
+  cudaGridDependencySynchronize();
+  join_weights(F, partial, rows, dweight, dbias, blockIdx.x);
+}
+
+// Short graphs: sums, A and B and the results in one launch.  graph_sums[graph][channel] = (sum of d, sum of d hat), or, for
+// one graph, the gradients themselves.
+template <typename X, typename Y, int ACT, int VEC>
+__global__ void __launch_bounds__(kNormThreads, VEC == 8 ? 1 : 2)
+    norm_graph_bwd_kernel(NormArgs a, GraphShape sh, float2* graph_sums, float* dweight, float* dbias) {
+  __shared__ float2 parts[kNormThreads * VEC], group_sums[kTileGroups], group_means[kTileGroups];
+  graph_kernel_begins();
+  const GraphPlace at = graph_place(a, sh);
+  const int32_t rows = (int32_t)(at.rows.hi - at.rows.lo), y0 = threadIdx.x / sh.across;
+  const int32_t chunk = at.step * kRows, chunks = (rows + chunk - 1) / chunk;
+  const int64_t base = at.rows.lo * a.F + at.channel;
+  const X* x = static_cast<const X*>(a.X) + base;
+  const Y* dy = static_cast<const Y*>(a.dY) + base;
+  X* dx = static_cast<X*>(a.out) + base;
+  const bool mine = at.channel < a.F;
+  Fixed<VEC> f = {};
+  if (mine) f = fixed_of<VEC>(a, at.graph, at.channel);
+  RawChannels<X, VEC> v[kRows];
+  RawChannels<Y, VEC> d[kRows];
+  auto load = [&](int32_t r0) {
 #pragma unroll
-  for (int o = 16; o > 0; o >>= 1) {
-    s1 += __shfl_xor_sync(0xffffffffu, s1, o);
-    s2 += __shfl_xor_sync(0xffffffffu, s2, o);
+    for (int u = 0; u < kRows; ++u) {
+      const int32_t r = r0 + u * at.step;
+      if (r < rows) {
+        v[u] = load_raw<X, VEC>(x + (int64_t)r * a.F);
+        d[u] = load_raw<Y, VEC>(dy + (int64_t)r * a.F);
+      }
+    }
+  };
+  float2 total[VEC] = {};
+  if (mine) {
+    for (int32_t c = 0; c < chunks; ++c) {
+      const int32_t r0 = c * chunk + at.y;
+      load(r0);
+      float2 s[VEC] = {};
+#pragma unroll
+      for (int u = 0; u < kRows; ++u) {
+        if (r0 + u * at.step >= rows) break;
+        const Channels<VEC> vx = numbers_of(v[u]), vd = numbers_of(d[u]);
+#pragma unroll
+        for (int k = 0; k < VEC; ++k) {
+          const float q = before_activation<ACT>(vd.v[k], vx.v[k], f.mean[k], f.rstd[k], f.w[k], f.b[k]);
+          s[k].x += q;
+          s[k].y = fmaf(q, (vx.v[k] - f.mean[k]) * f.rstd[k], s[k].y);
+        }
+      }
+#pragma unroll
+      for (int k = 0; k < VEC; ++k) {
+        total[k].x += s[k].x;
+        total[k].y += s[k].y;
+      }
+    }
   }
-  if (lane == 0) {
-    if (dbias) dbias[c] = (float)s1;
-    if (dweight) dweight[c] = (float)s2;
+  // parts[channel of the tile] behind the first `across` threads' vectors: sums over the block's rows
+#pragma unroll
+  for (int k = 0; k < VEC; ++k) parts[threadIdx.x * VEC + k] = total[k];
+  int half = 1;
+  while (half < sh.down) half *= 2;
+  for (half /= 2; half > 0; half /= 2) {
+    __syncthreads();
+    const int other = threadIdx.x + half * sh.across;
+    if (y0 < half && y0 + half < sh.down) {
+#pragma unroll
+      for (int k = 0; k < VEC; ++k) {
+        const float2 o = parts[other * VEC + k];
+        total[k].x += o.x;
+        total[k].y += o.y;
+        parts[threadIdx.x * VEC + k] = total[k];
+      }
+    }
   }
+  __syncthreads();
+  const int lane = threadIdx.x & 31, warp = threadIdx.x / 32;
+  const int32_t groups = at.tile_channels / a.width;
+  for (int32_t g = warp; g < groups; g += kNormThreads / 32) {
+    float s1 = 0.f, s2 = 0.f;
+    for (int32_t k = lane; k < a.width; k += 32) {
+      const float2 p = parts[g * a.width + k];
+      const float w = a.weight ? a.weight[at.tile_first + g * a.width + k] : 1.f;
+      s1 = fmaf(w, p.x, s1);
+      s2 = fmaf(w, p.y, s2);
+    }
+    s1 = warp_total(s1);
+    s2 = warp_total(s2);
+    if (lane == 0) group_sums[g] = make_float2(s1, s2);
+  }
+  if (sh.cluster > 1) {
+    cluster_arrive();
+    cluster_wait();
+  }
+  __syncthreads();
+  const float n = rows > 0 ? (float)rows * a.width : 1.f;
+  for (int32_t g = threadIdx.x; g < groups; g += kNormThreads) {
+    float2 s = group_sums[g];
+    if (sh.cluster > 1) {
+      s = make_float2(0.f, 0.f);
+      for (int32_t r = 0; r < sh.cluster; ++r) {
+        const float2 o = of_rank(group_sums + g, r);
+        s.x += o.x;
+        s.y += o.y;
+      }
+    }
+    group_means[g] = make_float2(s.x / n, s.y / n);
+  }
+  if (at.rank == 0 && (dweight || dbias)) {
+    for (int32_t k = threadIdx.x; k < at.tile_channels; k += kNormThreads) {
+      float2 s = parts[k];
+      for (int32_t r = 1; r < sh.cluster; ++r) {
+        const float2 o = of_rank(parts + k, r);
+        s.x += o.x;
+        s.y += o.y;
+      }
+      const int32_t channel = at.tile_first + k;
+      if (graph_sums) {
+        graph_sums[(int64_t)at.graph * a.F + channel] = s;
+      } else {
+        if (dbias) dbias[channel] = s.x;
+        if (dweight) dweight[channel] = s.y;
+      }
+    }
+  }
+  if (sh.cluster > 1) cluster_arrive();  // the others' shared memory has been read
+  __syncthreads();
+  if (mine && a.out) {
+    float A[VEC], B[VEC];
+#pragma unroll
+    for (int k = 0; k < VEC; ++k) {
+      const float2 m = group_means[(at.channel - at.tile_first + k) / a.width];
+      A[k] = m.x, B[k] = m.y;
+    }
+    for (int32_t c = chunks - 1; c >= 0; --c) {
+      const int32_t r0 = c * chunk + at.y;
+      if (c < chunks - 1) load(r0);
+#pragma unroll
+      for (int u = 0; u < kRows; ++u) {
+        if (r0 + u * at.step >= rows) break;
+        const Channels<VEC> vx = numbers_of(v[u]), vd = numbers_of(d[u]);
+        Channels<VEC> r;
+#pragma unroll
+        for (int k = 0; k < VEC; ++k) {
+          const float q = before_activation<ACT>(vd.v[k], vx.v[k], f.mean[k], f.rstd[k], f.w[k], f.b[k]) * f.w[k];
+          const float hat = (vx.v[k] - f.mean[k]) * f.rstd[k];
+          r.v[k] = (q - A[k] - hat * B[k]) * f.rstd[k];
+        }
+        store_channels<X, VEC>(dx + (int64_t)(r0 + u * at.step) * a.F, r);
+      }
+    }
+  }
+  if (sh.cluster > 1) cluster_wait();
+  graph_kernel_ends();
 }
 
 template <typename X, typename Y, int ACT, int VEC>
@@ -250,11 +417,27 @@ dg_status_t backward(const Graph* g, const NormArgs& a, dg_type_t x, dg_type_t y
   const bool weights = dweight || dbias;
   if (!weights && !a.out) return DG_OK;
   const int vec = norm_vector(a, x, y);
+  const unsigned weight_blocks = (unsigned)((a.F + 7) / 8);
+  void* memory = nullptr;
+  const GraphPlan plan = graph_plan(g, a, vec, sizeof(X), kRows);
+  const size_t graph_bytes = weights && plan.graphs > 1 ? (size_t)plan.graphs * a.F * sizeof(float2) : 0;
+  if (plan.graphs > 0 && (!graph_bytes || scratch_alloc(g, graph_bytes, s, &memory) == cudaSuccess)) {
+    float2* sums = static_cast<float2*>(memory);
+    cudaError_t e = by_vector<kWide>(vec, [&](auto v) {
+      return launch_graphs(plan, norm_graph_bwd_kernel<X, Y, ACT, decltype(v)::value>, s, a, sums, dweight, dbias);
+    });
+    if (e == cudaSuccess && sums)
+      e = launch_kernel(norm_weight_sums_kernel, dim3(weight_blocks), kJoinThreads, s, true, a.F, (const float2*)sums, plan.graphs,
+                        dweight, dbias);
+    pool_free(memory, s);
+    DG_CUDA(e);
+    count_launches((plan.long_graphs > 0) + (plan.graphs > plan.long_graphs) + (sums != nullptr));
+    return DG_OK;
+  }
   const NormShape sh = norm_shape(g, a, vec);
   const size_t partial_bytes = (size_t)sh.pieces * a.F * sizeof(float2);
   const int64_t pairs = a.out ? a.graphs * a.groups : 0;
-  void* memory = nullptr;
-  if (scratch_alloc(g, partial_bytes + (size_t)pairs * sizeof(float2), s, &memory) != cudaSuccess) {
+  if (plan.graphs > 0 || scratch_alloc(g, partial_bytes + (size_t)pairs * sizeof(float2), s, &memory) != cudaSuccess) {
     int across = 1;
     while (across < a.width && across < kNormThreads) across *= 2;
     if (weights)
@@ -273,19 +456,26 @@ dg_status_t backward(const Graph* g, const NormArgs& a, dg_type_t x, dg_type_t y
       norm_sums_kernel<X, Y, ACT, decltype(v)::value><<<grid, kNormThreads, 0, s>>>(a, sh, pieces, partial);
     });
   cudaError_t e = cudaGetLastError();
-  const int threads = a.graphs == 1 || sh.pieces / a.graphs * a.width > 64 ? kNormThreads : 32;
-  const int64_t blocks = pairs + (weights ? (a.F + threads / 32 - 1) / (threads / 32) : 0);
-  if (e == cudaSuccess)
-    e = launch_kernel(norm_join_sums_kernel, dim3((unsigned)blocks), threads, s, true, a, sh, g->batch_first,
-                      (const float2*)partial, a.out ? means : (float2*)nullptr, dweight, dbias);
+  int32_t lanes = 1;
+  while (lanes < a.width && lanes < 32) lanes *= 2;
+  const bool together = !pieces;  // one graph: the weights' blocks ride along
+  if (e == cudaSuccess && together)
+    e = launch_kernel(norm_join_sums_kernel, dim3((unsigned)pairs + (weights ? weight_blocks : 0)), kJoinThreads, s, true, a, sh,
+                      (const float2*)partial, a.out ? means : (float2*)nullptr, dweight, dbias, lanes);
+  if (e == cudaSuccess && !together && a.out)
+    e = launch_kernel(norm_join_means_kernel, dim3((unsigned)((pairs + 7) / 8)), kNormThreads, s, true, a, sh, g->batch_first,
+                      (const float2*)partial, means, lanes);
   if (e == cudaSuccess && a.out && sh.pieces > 0)
     e = by_vector<kWide>(vec, [&](auto v) {
       return launch_kernel(norm_apply_bwd_kernel<X, Y, ACT, decltype(v)::value>, grid, kNormThreads, s, true, a, sh, pieces,
                            (const float2*)means);
     });
+  if (e == cudaSuccess && !together && weights)
+    e = launch_kernel(norm_weight_sums_kernel, dim3(weight_blocks), kJoinThreads, s, true, a.F, (const float2*)partial,
+                      (int64_t)sh.pieces, dweight, dbias);
   pool_free(memory, s);
   DG_CUDA(e);
-  count_launches(1 + (sh.pieces > 0) + (a.out && sh.pieces > 0));
+  count_launches((sh.pieces > 0) + (together ? 1 : weights + (a.out != nullptr)) + (a.out && sh.pieces > 0));
   return DG_OK;
 }
 
