@@ -23,19 +23,22 @@ __device__ __forceinline__ void join(float& n, Moments& a, float nb, Moments b) 
   n = total;
 }
 
-// Adds `rows` of kStatRows rows (the rest are zeros) to a thread's moments: of a channel, or, with SHARED, of a vector of
+// Adds `rows` of kStep rows (the rest are zeros) to a thread's moments: of a channel, or, with SHARED, of a vector of
 // channels of one group.  n: cells so far.
+constexpr int kStep = 4;
 template <int VEC, bool SHARED>
 constexpr int kUnits = SHARED ? 1 : VEC;
 template <int VEC, bool SHARED>
-__device__ __forceinline__ void add_rows(const Channels<VEC> (&v)[kStatRows], int rows, float& n, Moments (&m)[kUnits<VEC, SHARED>]) {
-  const float cells = (float)(SHARED ? rows * VEC : rows), inverse = 1.f / cells;
-  const float total = n + cells, share = cells / total;
+__device__ __forceinline__ void add_rows(const Channels<VEC>* v, int rows, float& n, Moments (&m)[kUnits<VEC, SHARED>]) {
+  constexpr int kCells = SHARED ? VEC : 1;
+  const bool full = rows >= kStep;
+  const float cells = (float)(full ? kStep * kCells : rows * kCells), inverse = full ? 1.f / (kStep * kCells) : 1.f / cells;
+  const float total = n + cells, share = __fdividef(cells, total);
 #pragma unroll
   for (int k = 0; k < kUnits<VEC, SHARED>; ++k) {
     float sum = 0.f;
 #pragma unroll
-    for (int u = 0; u < kStatRows; ++u) {
+    for (int u = 0; u < kStep; ++u) {
       if constexpr (SHARED) {
 #pragma unroll
         for (int c = 0; c < VEC; ++c) sum += v[u].v[c];
@@ -46,19 +49,19 @@ __device__ __forceinline__ void add_rows(const Channels<VEC> (&v)[kStatRows], in
     const float mean = sum * inverse;
     float m2 = 0.f;
 #pragma unroll
-    for (int u = 0; u < kStatRows; ++u) {
-      if (u < rows) {
-        if constexpr (SHARED) {
+    for (int u = 0; u < kStep; ++u) {
+      float part = 0.f;
+      if constexpr (SHARED) {
 #pragma unroll
-          for (int c = 0; c < VEC; ++c) m2 = fmaf(v[u].v[c] - mean, v[u].v[c] - mean, m2);
-        } else {
-          m2 = fmaf(v[u].v[k] - mean, v[u].v[k] - mean, m2);
-        }
+        for (int c = 0; c < VEC; ++c) part = fmaf(v[u].v[c] - mean, v[u].v[c] - mean, part);
+      } else {
+        part = (v[u].v[k] - mean) * (v[u].v[k] - mean);
       }
+      m2 += u < rows ? part : 0.f;
     }
     const float d = mean - m[k].mean;
     m[k].mean = fmaf(d, share, m[k].mean);
-    m[k].m2 += m2 + d * d * (n * share);
+    m[k].m2 += fmaf(d * d, n * share, m2);
   }
   n = total;
 }
@@ -116,6 +119,7 @@ __global__ void __launch_bounds__(kNormThreads, VEC == 8 ? 2 : 4)
         }
       }
       add_rows<VEC, SHARED>(v, rows, n, m);
+      if (rows > kStep) add_rows<VEC, SHARED>(v + kStep, rows - kStep, n, m);
     }
   }
   join_block<kEach>(n, m, parts, counts, sh.across, sh.down);
@@ -127,107 +131,128 @@ __global__ void __launch_bounds__(kNormThreads, VEC == 8 ? 2 : 4)
   }
 }
 
-// Short graphs: statistics and results in one launch.
+// Short graphs: statistics and results in one launch.  What every block costs beside its cells counts here: sums over the
+// block are plain ones (the mean, then the squares about it), one warp for a group.
 template <typename X, typename Y, int ACT, int VEC, bool SHARED>
 __global__ void __launch_bounds__(kNormThreads, VEC == 8 ? 2 : 3) norm_graph_kernel(NormArgs a, GraphShape sh) {
   constexpr int kEach = kUnits<VEC, SHARED>;
   __shared__ Moments parts[kNormThreads * kEach];
   __shared__ float counts[kNormThreads];
-  __shared__ float2 group_parts[kTileGroups], group_stats[kTileGroups];
+  __shared__ float2 group_parts[kTileGroups], group_stats[kTileGroups], block_cells;
   graph_kernel_begins();
   const GraphPlace at = graph_place(a, sh);
-  const int32_t rows = (int32_t)(at.rows.hi - at.rows.lo);
-  const int32_t chunk = at.step * kStatRows, chunks = (rows + chunk - 1) / chunk;
-  const int64_t base = at.rows.lo * a.F + at.channel;
-  const X* x = static_cast<const X*>(a.X) + base;
-  Y* y = static_cast<Y*>(a.out) + base;
+  const int32_t chunk = at.step * kStatRows;
+  const X* x = static_cast<const X*>(a.X) + at.base;
+  Y* y = static_cast<Y*>(a.out) + at.base;
   const bool mine = at.channel < a.F;
   RawChannels<X, VEC> raw[kStatRows];
   auto load = [&](int32_t r0) {
 #pragma unroll
     for (int u = 0; u < kStatRows; ++u) {
       raw[u] = RawChannels<X, VEC>{};
-      if (r0 + u * at.step < rows) raw[u] = load_raw<X, VEC>(x + (int64_t)(r0 + u * at.step) * a.F);
+      if (at.row + r0 + u * at.step < at.rows) raw[u] = load_raw<X, VEC>(x + (int64_t)(r0 + u * at.step) * a.F);
     }
   };
   Moments m[kEach] = {};
-  float n = 0.f;
+  float n = 0.f, w[VEC], b[VEC];
+  int32_t last = 0;  // the chunk that stays in registers
   if (mine) {
-    for (int32_t c = 0; c < chunks; ++c) {
-      const int32_t r0 = c * chunk + at.y;
+#pragma unroll
+    for (int c = 0; c < VEC; ++c) {
+      w[c] = a.weight ? a.weight[at.channel + c] : 1.f;
+      b[c] = a.bias ? a.bias[at.channel + c] : 0.f;
+    }
+    for (int32_t r0 = 0; at.row + r0 < at.rows; r0 += chunk) {
+      last = r0;
       load(r0);
-      if (r0 >= rows) break;  // of the last chunk: it stays in `raw` for what follows, as nothing
       Channels<VEC> v[kStatRows];
       int count = 0;
 #pragma unroll
       for (int u = 0; u < kStatRows; ++u) {
         v[u] = numbers_of(raw[u]);
-        count += r0 + u * at.step < rows;
+        count += at.row + r0 + u * at.step < at.rows;
       }
       add_rows<VEC, SHARED>(v, count, n, m);
+      if (count > kStep) add_rows<VEC, SHARED>(v + kStep, count - kStep, n, m);
     }
   }
-  join_block<kEach>(n, m, parts, counts, sh.across, sh.down);
+  // parts[y][unit of the tile], and the cells of each in counts[y]
+  if (at.y < sh.down) {
+#pragma unroll
+    for (int k = 0; k < kEach; ++k) parts[threadIdx.x * kEach + k] = m[k];
+    if (at.x == 0) counts[at.y] = n;
+  }
   __syncthreads();
-  // a warp for a group: its units have the same count each
   const int lane = threadIdx.x & 31, warp = threadIdx.x / 32;
-  const int32_t groups = at.tile_channels / a.width, units = SHARED ? a.width / VEC : a.width;
-  const float count = (float)rows_of_rank(at, sh, at.rank) * (SHARED ? VEC : 1);
-  auto unit = [&](int32_t g, int32_t k) {
-    const int32_t u = g * units + k;
-    return SHARED ? parts[u] : parts[u % VEC * kNormThreads + u / VEC];
-  };
+  const int32_t groups = group_of(sh, at.tile_channels - 1) + 1, units = SHARED ? a.width / VEC : a.width;
+  const int32_t lanes = 1 << sh.lanes_log, y0 = lane >> sh.lanes_log, stride = sh.across * kEach;
   for (int32_t g = warp; g < groups; g += kNormThreads / 32) {
-    float sum = 0.f;
-    for (int32_t k = lane; k < units; k += 32) sum += unit(g, k).mean;
-    const float mean = warp_total(sum) / units;
-    sum = 0.f;
-    for (int32_t k = lane; k < units; k += 32) {
-      const Moments u = unit(g, k);
-      sum += fmaf(count * (u.mean - mean), u.mean - mean, u.m2);
+    float sum = 0.f, total = 0.f;
+    for (int32_t yy = y0; yy < sh.down; yy += 32 >> sh.lanes_log) {
+      const float c = counts[yy];
+      for (int32_t k = lane & (lanes - 1); k < units; k += lanes) {
+        sum = fmaf(c, parts[yy * stride + g * units + k].mean, sum);
+        total += c;
+      }
     }
     sum = warp_total(sum);
-    if (lane == 0) group_parts[g] = make_float2(mean, sum);
+    total = warp_total(total);
+    const float mean = total > 0.f ? sum / total : 0.f;
+    float squares = 0.f;
+    for (int32_t yy = y0; yy < sh.down; yy += 32 >> sh.lanes_log) {
+      const float c = counts[yy];
+      for (int32_t k = lane & (lanes - 1); k < units; k += lanes) {
+        const Moments u = parts[yy * stride + g * units + k];
+        const float d = u.mean - mean;
+        squares += c > 0.f ? fmaf(c * d, d, u.m2) : 0.f;
+      }
+    }
+    squares = warp_total(squares);
+    if (lane == 0) {
+      group_parts[g] = make_float2(mean, squares);
+      if (g == 0) block_cells = make_float2(total, 0.f);  // of any group
+    }
   }
-  if (sh.cluster > 1) {
+  if (sh.cluster_log > 0) {
     cluster_arrive();
     cluster_wait();
   }
   __syncthreads();
-  const float cells = rows > 0 ? (float)rows * a.width : 1.f;
   for (int32_t g = threadIdx.x; g < groups; g += kNormThreads) {
     float2 p = group_parts[g];
-    if (sh.cluster > 1) {
+    if (sh.cluster_log > 0) {
       // the blocks' parts, in the order of their ranks
-      float part_cells = 0.f;
+      float cells = 0.f;
       Moments all = {0.f, 0.f};
-      for (int32_t r = 0; r < sh.cluster; ++r) {
+      for (int32_t r = 0; r < 1 << sh.cluster_log; ++r) {
         const float2 o = of_rank(group_parts + g, r);
-        join(part_cells, all, (float)rows_of_rank(at, sh, r) * a.width, Moments{o.x, o.y});
+        join(cells, all, of_rank(&block_cells, r).x, Moments{o.x, o.y});
       }
       p = make_float2(all.mean, all.m2);
     }
+    const float cells = at.rows > 0 ? (float)at.rows * a.width : 1.f;
     const float2 st = make_float2(p.x, 1.f / sqrtf(p.y / cells + a.eps));
     group_stats[g] = st;
     if (at.rank == 0) a.stats[(int64_t)at.graph * a.groups + at.tile_first / a.width + g] = st;
   }
-  if (sh.cluster > 1) cluster_arrive();  // the others' shared memory has been read
+  if (sh.cluster_log > 0) cluster_arrive();  // the others' shared memory has been read
   __syncthreads();
   if (mine) {
-    float mean[VEC], rstd[VEC], w[VEC], b[VEC];
+    float mean[VEC], rstd[VEC];
 #pragma unroll
     for (int c = 0; c < VEC; ++c) {
-      const float2 st = group_stats[(at.channel - at.tile_first + c) / a.width];
-      mean[c] = st.x, rstd[c] = st.y;
-      w[c] = a.weight ? a.weight[at.channel + c] : 1.f;
-      b[c] = a.bias ? a.bias[at.channel + c] : 0.f;
+      if (c == 0 || !SHARED) {
+        const float2 st = group_stats[group_of(sh, at.channel - at.tile_first + c)];
+        mean[c] = st.x, rstd[c] = st.y;
+      } else {
+        mean[c] = mean[0], rstd[c] = rstd[0];
+      }
     }
-    for (int32_t c = chunks - 1; c >= 0; --c) {
-      const int32_t r0 = c * chunk + at.y;
-      if (c < chunks - 1) load(r0);
+    for (int32_t r0 = last; r0 >= 0; r0 -= chunk) {
+      if (r0 < last) load(r0);
 #pragma unroll
       for (int u = 0; u < kStatRows; ++u) {
-        if (r0 + u * at.step >= rows) break;
+        if (at.row + r0 + u * at.step >= at.rows) break;
         Channels<VEC> v = numbers_of(raw[u]);
 #pragma unroll
         for (int k = 0; k < VEC; ++k) v.v[k] = activated<ACT>(fmaf((v.v[k] - mean[k]) * rstd[k], w[k], b[k]));
@@ -235,7 +260,7 @@ __global__ void __launch_bounds__(kNormThreads, VEC == 8 ? 2 : 3) norm_graph_ker
       }
     }
   }
-  if (sh.cluster > 1) cluster_wait();
+  if (sh.cluster_log > 0) cluster_wait();
   graph_kernel_ends();
 }
 
@@ -341,7 +366,7 @@ template <typename X, typename Y, int ACT>
 dg_status_t forward(const Graph* g, const NormArgs& a, dg_type_t x, dg_type_t y, cudaStream_t s) {
   const int vec = norm_vector(a, x, y);
   const bool shared = vec > 1 && a.width % vec == 0;
-  if (const GraphPlan plan = graph_plan(g, a, vec, sizeof(X), kStatRows); plan.graphs > 0) {
+  if (const GraphPlan plan = graph_plan(g, a, vec, sizeof(X), kStatRows, shared); plan.graphs > 0) {
     DG_CUDA((by_vector<sizeof(X) == 2 && sizeof(Y) == 2>(vec, [&](auto v) {
       constexpr int VEC = decltype(v)::value;
       return shared ? launch_graphs(plan, norm_graph_kernel<X, Y, ACT, VEC, true>, s, a)
@@ -404,9 +429,10 @@ int norm_vector(const NormArgs& a, dg_type_t x, dg_type_t y) {
   return vec;
 }
 
-GraphPlan graph_plan(const Graph* g, const NormArgs& a, int vec, int x_bytes, int rows_kept) {
+GraphPlan graph_plan(const Graph* g, const NormArgs& a, int vec, int x_bytes, int rows_kept, bool shared) {
+  // bytes of a graph in a tile: up to kShort one block takes them, up to kLong a cluster
+  constexpr int64_t kShort = 256 << 10, kLong = 1 << 20;
   GraphPlan plan{};
-  GraphShape& sh = plan.shape;
   const int64_t longest = g->batch_longest < 0 ? g->n : g->batch_longest;
   const int32_t vectors = a.F / vec;
   // the fewest vectors that whole groups fill
@@ -414,33 +440,48 @@ GraphPlan graph_plan(const Graph* g, const NormArgs& a, int vec, int x_bytes, in
   while (least % vec) least += a.width;
   least /= vec;
   if (least > kNormThreads) return plan;
-  // lines of 128 bytes, or sectors of 32 where the graphs are few
-  auto tile = [&](int bytes) {
+  auto shape = [&](int32_t across, int cluster_log) {
+    GraphShape sh{};
+    sh.vec = vec;
+    const int32_t parts = vectors / least, tiles = (vectors + across - 1) / across;  // of even width
+    sh.across = (parts + tiles - 1) / tiles * least;
+    sh.by_across = (65536 + sh.across - 1) / sh.across;
+    sh.down = kNormThreads / sh.across;
+    sh.tiles = (vectors + sh.across - 1) / sh.across;
+    sh.cluster_log = cluster_log;
+    const int32_t units = shared ? a.width / vec : a.width;
+    while (sh.lanes_log < 5 && (1 << sh.lanes_log) < units) ++sh.lanes_log;
+    sh.by_width = 1.f / a.width;
+    sh.order = g->batch_order;
+    return sh;
+  };
+  // Long graphs: lines of 128 bytes, or sectors of 32 where the graphs are few; their rows are spread over a cluster.
+  auto narrow = [&](int bytes) {
     int32_t across = least;
     while (across * vec * x_bytes < bytes && across + least <= vectors && across + least <= kNormThreads) across += least;
     return across;
   };
-  sh.across = tile(128);
-  if (a.graphs * (vectors / sh.across) < g->sm_count) sh.across = tile(32);
-  sh.vec = vec;
-  sh.down = kNormThreads / sh.across;
-  sh.tiles = (vectors + sh.across - 1) / sh.across;
-  sh.order = g->batch_order;
-  const int64_t kept = (int64_t)sh.down * rows_kept;  // rows in a block's registers
-  if (longest > 4 * kCluster * kept) return plan;
-  if (a.graphs * sh.tiles * kCluster >= ((int64_t)1 << 31)) return plan;
+  int32_t across = narrow(128);
+  if (a.graphs * (vectors / across) < g->sm_count) across = narrow(32);
+  plan.shape[0] = shape(across, kClusterLog);
+  if (plan.shape[0].tiles > 65535 || longest * plan.shape[0].across * vec * x_bytes > kLong) return plan;
+  if (a.graphs << kClusterLog >= (int64_t)1 << 31) return plan;
   plan.graphs = a.graphs;
-  if (!g->batch_lengths) {
-    plan.long_graphs = 1;
-  } else {
-    // graphs, longest first, of more than two registerfuls of a block
-    int64_t lo = 0, hi = a.graphs;
-    while (lo < hi) {
-      const int64_t mid = (lo + hi) / 2;
-      if (g->batch_lengths[mid] > 2 * kept) lo = mid + 1; else hi = mid;
-    }
-    plan.long_graphs = lo;
+  plan.long_graphs = 1;
+  if (!g->batch_lengths) return plan;
+  // The others: as wide as leaves an average graph four registerfuls of a block at most.  2048 graphs of 1 to 2500 rows of
+  // 128: TIME
+  auto fits = [&](int32_t wide) { return 4 * (int64_t)(kNormThreads / wide) * rows_kept * a.graphs >= a.rows; };
+  while (across + least <= vectors && across + least <= kNormThreads && fits(across + least)) across += least;
+  plan.shape[1] = shape(across, 0);
+  const int64_t most = kShort / ((int64_t)plan.shape[1].across * vec * x_bytes);
+  int64_t lo = 0, hi = a.graphs;
+  while (lo < hi) {
+    const int64_t mid = (lo + hi) / 2;
+    if (g->batch_lengths[mid] > most) lo = mid + 1; else hi = mid;
   }
+  plan.long_graphs = lo;
+  plan.shape[1].first = (int32_t)lo;
   return plan;
 }
 

@@ -271,48 +271,53 @@ __device__ __forceinline__ double block_sum(double v) {
 
 // A cluster of blocks takes the rows of one graph in the channels of a tile, which holds whole groups: what it sums it
 // needs nowhere else, and rows that fit its registers are read once.
-constexpr int kCluster = 8;
+constexpr int kClusterLog = 3;
 constexpr int kTileGroups = 128;  // most groups of a tile
 struct GraphShape {
   int32_t vec, across, down, tiles;
-  int32_t cluster;       // blocks: 1 or kCluster
+  uint32_t by_across;    // thread / across = thread * by_across >> 16
+  int32_t cluster_log;   // log2 of the blocks
+  int32_t lanes_log;     // log2 of the threads along a group's units, at most 5
+  float by_width;        // 1 / width: groups of a tile's channels
   int32_t first;         // place in `order` of the launch's first graph
   const int32_t* order;  // graphs, longest first; null: one graph
 };
 // A call's two launches: long graphs, then the others.
 struct GraphPlan {
-  GraphShape shape;
+  GraphShape shape[2];
   int64_t long_graphs, graphs;  // 0 graphs: not a call for these kernels
 };
-GraphPlan graph_plan(const Graph* g, const NormArgs& a, int vec, int x_bytes, int rows_kept);
+GraphPlan graph_plan(const Graph* g, const NormArgs& a, int vec, int x_bytes, int rows_kept, bool shared);
 
 struct GraphPlace {
-  int32_t graph, rank, cluster;
+  int32_t graph, rank;
   int32_t channel, tile_channels;  // the thread's first channel (>= F: none), those of the tile
   int32_t tile_first;
-  int32_t y, step;                 // its first row of the graph, and the distance to its next
-  Rows rows;
+  int32_t x, y;                    // its place in the block: along the tile's vectors, along the rows
+  int32_t row, step;               // its first row of the graph, and the distance to its next
+  int32_t rows;
+  int64_t base;                    // of that row's first channel, in numbers
 };
 __device__ __forceinline__ GraphPlace graph_place(const NormArgs& a, const GraphShape& sh) {
   GraphPlace r;
-  r.cluster = sh.cluster;
-  const int64_t item = blockIdx.x / sh.cluster;
-  r.rank = (int32_t)(blockIdx.x % sh.cluster);
-  const int32_t at = sh.first + (int32_t)(item / sh.tiles), tile = (int32_t)(item % sh.tiles);
+  const int32_t at = sh.first + (blockIdx.x >> sh.cluster_log);
+  r.rank = blockIdx.x & ((1 << sh.cluster_log) - 1);
   r.graph = sh.order ? sh.order[at] : 0;
-  r.rows = rows_of(a, r.graph);
-  r.tile_first = tile * sh.across * sh.vec;
+  const Rows rows = rows_of(a, r.graph);
+  r.rows = (int32_t)(rows.hi - rows.lo);
+  r.tile_first = blockIdx.y * sh.across * sh.vec;
   r.tile_channels = min(sh.across * sh.vec, a.F - r.tile_first);
-  const int32_t y = threadIdx.x / sh.across, x = threadIdx.x % sh.across * sh.vec;
-  r.channel = y < sh.down && x < r.tile_channels ? r.tile_first + x : a.F;
-  r.y = r.rank * sh.down + y;
-  r.step = sh.cluster * sh.down;
+  r.y = threadIdx.x * sh.by_across >> 16;
+  r.x = threadIdx.x - r.y * sh.across;
+  r.channel = r.y < sh.down && r.x * sh.vec < r.tile_channels ? r.tile_first + r.x * sh.vec : a.F;
+  r.row = r.rank * sh.down + r.y;
+  r.step = sh.down << sh.cluster_log;
+  r.base = (rows.lo + r.row) * a.F + r.channel;
   return r;
 }
-// Rows that a block of the cluster has.
-__device__ __forceinline__ int32_t rows_of_rank(const GraphPlace& at, const GraphShape& sh, int32_t rank) {
-  const int32_t rows = (int32_t)(at.rows.hi - at.rows.lo), rest = rows % at.step - rank * sh.down;
-  return rows / at.step * sh.down + min(max(rest, 0), sh.down);
+// The group of a channel of the tile: at most 2048 channels, so that the product is off by less than 1 / (2 width).
+__device__ __forceinline__ int32_t group_of(const GraphShape& sh, int32_t channel) {
+  return (int32_t)((channel + 0.5f) * sh.by_width);
 }
 __device__ __forceinline__ void cluster_arrive() { asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory"); }
 __device__ __forceinline__ void cluster_wait() { asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory"); }
@@ -333,7 +338,7 @@ __device__ __forceinline__ float warp_total(float v) {
 // The launch of the other graphs may begin once all blocks of this one have; it ends behind it, by its last block.
 __device__ __forceinline__ void graph_kernel_begins() { cudaTriggerProgrammaticLaunchCompletion(); }
 __device__ __forceinline__ void graph_kernel_ends() {
-  if (blockIdx.x == gridDim.x - 1) cudaGridDependencySynchronize();
+  if (blockIdx.x == gridDim.x - 1 && blockIdx.y == gridDim.y - 1) cudaGridDependencySynchronize();
 }
 
 // Both launches of a plan.
@@ -344,17 +349,15 @@ cudaError_t launch_graphs(const GraphPlan& plan, void (*kernel)(NormArgs, GraphS
   bool before = false;
   for (int i = 0; i < 2; ++i) {
     if (counts[i] == 0) continue;
-    GraphShape sh = plan.shape;
-    sh.cluster = i == 0 ? kCluster : 1;
-    sh.first = i == 0 ? 0 : (int32_t)plan.long_graphs;
+    const GraphShape& sh = plan.shape[i];
     cudaLaunchAttribute attributes[2] = {};
     attributes[0].id = cudaLaunchAttributeClusterDimension;
-    attributes[0].val.clusterDim.x = (unsigned)sh.cluster;
+    attributes[0].val.clusterDim.x = 1u << sh.cluster_log;
     attributes[0].val.clusterDim.y = attributes[0].val.clusterDim.z = 1;
     attributes[1].id = cudaLaunchAttributeProgrammaticStreamSerialization;
     attributes[1].val.programmaticStreamSerializationAllowed = 1;
     cudaLaunchConfig_t config{};
-    config.gridDim = dim3((unsigned)(counts[i] * sh.tiles * sh.cluster));
+    config.gridDim = dim3((unsigned)(counts[i] << sh.cluster_log), (unsigned)sh.tiles);
     config.blockDim = dim3(kNormThreads);
     config.stream = s;
     config.attrs = attributes;

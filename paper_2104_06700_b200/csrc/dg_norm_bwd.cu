@@ -158,36 +158,44 @@ __global__ void __launch_bounds__(kNormThreads, VEC == 8 ? 1 : 2)
   __shared__ float2 parts[kNormThreads * VEC], group_sums[kTileGroups], group_means[kTileGroups];
   graph_kernel_begins();
   const GraphPlace at = graph_place(a, sh);
-  const int32_t rows = (int32_t)(at.rows.hi - at.rows.lo), y0 = threadIdx.x / sh.across;
-  const int32_t chunk = at.step * kRows, chunks = (rows + chunk - 1) / chunk;
-  const int64_t base = at.rows.lo * a.F + at.channel;
-  const X* x = static_cast<const X*>(a.X) + base;
-  const Y* dy = static_cast<const Y*>(a.dY) + base;
-  X* dx = static_cast<X*>(a.out) + base;
+  const int32_t chunk = at.step * kRows, first_group = at.tile_first / a.width;
+  const X* x = static_cast<const X*>(a.X) + at.base;
+  const Y* dy = static_cast<const Y*>(a.dY) + at.base;
+  X* dx = static_cast<X*>(a.out) + at.base;
   const bool mine = at.channel < a.F;
+  int32_t group[VEC];
   Fixed<VEC> f = {};
-  if (mine) f = fixed_of<VEC>(a, at.graph, at.channel);
+  if (mine) {
+#pragma unroll
+    for (int k = 0; k < VEC; ++k) {
+      group[k] = group_of(sh, at.channel - at.tile_first + k);
+      const float2 st = a.stats[(int64_t)at.graph * a.groups + first_group + group[k]];
+      f.mean[k] = st.x, f.rstd[k] = st.y;
+      f.w[k] = a.weight ? a.weight[at.channel + k] : 1.f;
+      f.b[k] = a.bias ? a.bias[at.channel + k] : 0.f;
+    }
+  }
   RawChannels<X, VEC> v[kRows];
   RawChannels<Y, VEC> d[kRows];
   auto load = [&](int32_t r0) {
 #pragma unroll
     for (int u = 0; u < kRows; ++u) {
-      const int32_t r = r0 + u * at.step;
-      if (r < rows) {
-        v[u] = load_raw<X, VEC>(x + (int64_t)r * a.F);
-        d[u] = load_raw<Y, VEC>(dy + (int64_t)r * a.F);
+      if (at.row + r0 + u * at.step < at.rows) {
+        v[u] = load_raw<X, VEC>(x + (int64_t)(r0 + u * at.step) * a.F);
+        d[u] = load_raw<Y, VEC>(dy + (int64_t)(r0 + u * at.step) * a.F);
       }
     }
   };
   float2 total[VEC] = {};
+  int32_t last = 0;  // the chunk that stays in registers
   if (mine) {
-    for (int32_t c = 0; c < chunks; ++c) {
-      const int32_t r0 = c * chunk + at.y;
+    for (int32_t r0 = 0; at.row + r0 < at.rows; r0 += chunk) {
+      last = r0;
       load(r0);
       float2 s[VEC] = {};
 #pragma unroll
       for (int u = 0; u < kRows; ++u) {
-        if (r0 + u * at.step >= rows) break;
+        if (at.row + r0 + u * at.step >= at.rows) break;
         const Channels<VEC> vx = numbers_of(v[u]), vd = numbers_of(d[u]);
 #pragma unroll
         for (int k = 0; k < VEC; ++k) {
@@ -203,50 +211,55 @@ __global__ void __launch_bounds__(kNormThreads, VEC == 8 ? 1 : 2)
       }
     }
   }
-  // parts[channel of the tile] behind the first `across` threads' vectors: sums over the block's rows
+  // parts[y][channel of the tile]
+  const int32_t stride = sh.across * VEC;
+  if (at.y < sh.down) {
 #pragma unroll
-  for (int k = 0; k < VEC; ++k) parts[threadIdx.x * VEC + k] = total[k];
-  int half = 1;
-  while (half < sh.down) half *= 2;
-  for (half /= 2; half > 0; half /= 2) {
-    __syncthreads();
-    const int other = threadIdx.x + half * sh.across;
-    if (y0 < half && y0 + half < sh.down) {
-#pragma unroll
-      for (int k = 0; k < VEC; ++k) {
-        const float2 o = parts[other * VEC + k];
-        total[k].x += o.x;
-        total[k].y += o.y;
-        parts[threadIdx.x * VEC + k] = total[k];
-      }
+    for (int k = 0; k < VEC; ++k) parts[threadIdx.x * VEC + k] = total[k];
+  }
+  __syncthreads();
+  // a channel's sum over the block's rows, in parts[0][channel]
+  for (int32_t k = threadIdx.x; k < at.tile_channels; k += kNormThreads) {
+    float2 s = parts[k];
+    for (int32_t yy = 1; yy < sh.down; ++yy) {
+      s.x += parts[yy * stride + k].x;
+      s.y += parts[yy * stride + k].y;
     }
+    parts[k] = s;
   }
   __syncthreads();
   const int lane = threadIdx.x & 31, warp = threadIdx.x / 32;
-  const int32_t groups = at.tile_channels / a.width;
-  for (int32_t g = warp; g < groups; g += kNormThreads / 32) {
+  const int32_t groups = group_of(sh, at.tile_channels - 1) + 1, lanes = 1 << sh.lanes_log;
+  // several groups a warp: `lanes` threads along the channels of each
+  for (int32_t g0 = warp * (32 >> sh.lanes_log); g0 < groups; g0 += (kNormThreads / 32) * (32 >> sh.lanes_log)) {
+    const int32_t g = g0 + (lane >> sh.lanes_log);
     float s1 = 0.f, s2 = 0.f;
-    for (int32_t k = lane; k < a.width; k += 32) {
-      const float2 p = parts[g * a.width + k];
-      const float w = a.weight ? a.weight[at.tile_first + g * a.width + k] : 1.f;
-      s1 = fmaf(w, p.x, s1);
-      s2 = fmaf(w, p.y, s2);
+    if (g < groups) {
+      for (int32_t k = lane & (lanes - 1); k < a.width; k += lanes) {
+        const float2 p = parts[g * a.width + k];
+        const float w = a.weight ? a.weight[at.tile_first + g * a.width + k] : 1.f;
+        s1 = fmaf(w, p.x, s1);
+        s2 = fmaf(w, p.y, s2);
+      }
     }
-    s1 = warp_total(s1);
-    s2 = warp_total(s2);
-    if (lane == 0) group_sums[g] = make_float2(s1, s2);
+    for (int o = lanes / 2; o > 0; o /= 2) {
+      s1 += __shfl_xor_sync(0xffffffffu, s1, o);
+      s2 += __shfl_xor_sync(0xffffffffu, s2, o);
+    }
+    if (g < groups && (lane & (lanes - 1)) == 0) group_sums[g] = make_float2(s1, s2);
   }
-  if (sh.cluster > 1) {
+  const int32_t cluster = 1 << sh.cluster_log;
+  if (cluster > 1) {
     cluster_arrive();
     cluster_wait();
   }
   __syncthreads();
-  const float n = rows > 0 ? (float)rows * a.width : 1.f;
   for (int32_t g = threadIdx.x; g < groups; g += kNormThreads) {
+    const float n = at.rows > 0 ? (float)at.rows * a.width : 1.f;
     float2 s = group_sums[g];
-    if (sh.cluster > 1) {
+    if (cluster > 1) {
       s = make_float2(0.f, 0.f);
-      for (int32_t r = 0; r < sh.cluster; ++r) {
+      for (int32_t r = 0; r < cluster; ++r) {
         const float2 o = of_rank(group_sums + g, r);
         s.x += o.x;
         s.y += o.y;
@@ -257,7 +270,7 @@ __global__ void __launch_bounds__(kNormThreads, VEC == 8 ? 1 : 2)
   if (at.rank == 0 && (dweight || dbias)) {
     for (int32_t k = threadIdx.x; k < at.tile_channels; k += kNormThreads) {
       float2 s = parts[k];
-      for (int32_t r = 1; r < sh.cluster; ++r) {
+      for (int32_t r = 1; r < cluster; ++r) {
         const float2 o = of_rank(parts + k, r);
         s.x += o.x;
         s.y += o.y;
@@ -271,21 +284,20 @@ __global__ void __launch_bounds__(kNormThreads, VEC == 8 ? 1 : 2)
       }
     }
   }
-  if (sh.cluster > 1) cluster_arrive();  // the others' shared memory has been read
+  if (cluster > 1) cluster_arrive();  // the others' shared memory has been read
   __syncthreads();
   if (mine && a.out) {
     float A[VEC], B[VEC];
 #pragma unroll
     for (int k = 0; k < VEC; ++k) {
-      const float2 m = group_means[(at.channel - at.tile_first + k) / a.width];
+      const float2 m = group_means[group[k]];
       A[k] = m.x, B[k] = m.y;
     }
-    for (int32_t c = chunks - 1; c >= 0; --c) {
-      const int32_t r0 = c * chunk + at.y;
-      if (c < chunks - 1) load(r0);
+    for (int32_t r0 = last; r0 >= 0; r0 -= chunk) {
+      if (r0 < last) load(r0);
 #pragma unroll
       for (int u = 0; u < kRows; ++u) {
-        if (r0 + u * at.step >= rows) break;
+        if (at.row + r0 + u * at.step >= at.rows) break;
         const Channels<VEC> vx = numbers_of(v[u]), vd = numbers_of(d[u]);
         Channels<VEC> r;
 #pragma unroll
@@ -298,7 +310,7 @@ __global__ void __launch_bounds__(kNormThreads, VEC == 8 ? 1 : 2)
       }
     }
   }
-  if (sh.cluster > 1) cluster_wait();
+  if (cluster > 1) cluster_wait();
   graph_kernel_ends();
 }
 
@@ -419,7 +431,7 @@ dg_status_t backward(const Graph* g, const NormArgs& a, dg_type_t x, dg_type_t y
   const int vec = norm_vector(a, x, y);
   const unsigned weight_blocks = (unsigned)((a.F + 7) / 8);
   void* memory = nullptr;
-  const GraphPlan plan = graph_plan(g, a, vec, sizeof(X), kRows);
+  const GraphPlan plan = graph_plan(g, a, vec, sizeof(X), kRows, false);
   const size_t graph_bytes = weights && plan.graphs > 1 ? (size_t)plan.graphs * a.F * sizeof(float2) : 0;
   if (plan.graphs > 0 && (!graph_bytes || scratch_alloc(g, graph_bytes, s, &memory) == cudaSuccess)) {
     float2* sums = static_cast<float2*>(memory);
