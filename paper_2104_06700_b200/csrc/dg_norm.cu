@@ -10,6 +10,8 @@ namespace {
 
 // Rows a thread has in flight, and takes the mean of before it joins that to what it has.
 constexpr int kStatRows = 8;
+// Rows of a thread in shared memory, in groups of kStep: with four blocks on an SM.
+constexpr int kStep = 4, kSlots = 12;
 
 // Count, mean and sum of squares about the mean; joined they lose nothing to large means, as sums of x and x^2 would.
 struct Moments {
@@ -25,7 +27,6 @@ __device__ __forceinline__ void join(float& n, Moments& a, float nb, Moments b) 
 
 // Adds `rows` of kStep rows (the rest are zeros) to a thread's moments: of a channel, or, with SHARED, of a vector of
 // channels of one group.  n: cells so far.
-constexpr int kStep = 4;
 template <int VEC, bool SHARED>
 constexpr int kUnits = SHARED ? 1 : VEC;
 template <int VEC, bool SHARED>
@@ -134,23 +135,25 @@ __global__ void __launch_bounds__(kNormThreads, VEC == 8 ? 2 : 4)
 // Short graphs: statistics and results in one launch.  What every block costs beside its cells counts here: sums over the
 // block are plain ones (the mean, then the squares about it), one warp for a group.
 template <typename X, typename Y, int ACT, int VEC, bool SHARED>
-__global__ void __launch_bounds__(kNormThreads, VEC == 8 ? 2 : 3) norm_graph_kernel(NormArgs a, GraphShape sh) {
+__global__ void __launch_bounds__(kNormThreads, VEC == 8 ? 3 : 4) norm_graph_kernel(const __grid_constant__ NormArgs a, const __grid_constant__ GraphPlan plan) {
   constexpr int kEach = kUnits<VEC, SHARED>;
   __shared__ Moments parts[kNormThreads * kEach];
   __shared__ float counts[kNormThreads];
   __shared__ float2 group_parts[kTileGroups], group_stats[kTileGroups], block_cells;
-  graph_kernel_begins();
-  const GraphPlace at = graph_place(a, sh);
-  const int32_t chunk = at.step * kStatRows;
+  const bool is_long = blockIdx.x < plan.long_blocks;
+  const GraphShape sh = is_long ? plan.shape[0] : plan.shape[1];
+  const GraphPlace at = graph_place(a, plan, sh, is_long);
+  const int32_t chunk = at.step * kSlots;
   const X* x = static_cast<const X*>(a.X) + at.base;
   Y* y = static_cast<Y*>(a.out) + at.base;
   const bool mine = at.channel < a.F;
-  RawChannels<X, VEC> raw[kStatRows];
+  extern __shared__ uint4 slots[];
+  RawChannels<X, VEC>* const slot = reinterpret_cast<RawChannels<X, VEC>*>(slots) + threadIdx.x;
   auto load = [&](int32_t r0) {
 #pragma unroll
-    for (int u = 0; u < kStatRows; ++u) {
-      raw[u] = RawChannels<X, VEC>{};
-      if (at.row + r0 + u * at.step < at.rows) raw[u] = load_raw<X, VEC>(x + (int64_t)(r0 + u * at.step) * a.F);
+    for (int u = 0; u < kSlots; ++u) {
+      if (at.row + r0 + u * at.step < at.rows) fetch<X, VEC>(slot + u * kNormThreads, x + (int64_t)(r0 + u * at.step) * a.F);
+      if (u % kStep == kStep - 1) fetch_group();
     }
   };
   Moments m[kEach] = {};
@@ -165,15 +168,26 @@ __global__ void __launch_bounds__(kNormThreads, VEC == 8 ? 2 : 3) norm_graph_ker
     for (int32_t r0 = 0; at.row + r0 < at.rows; r0 += chunk) {
       last = r0;
       load(r0);
-      Channels<VEC> v[kStatRows];
-      int count = 0;
+      auto take = [&](int first) {
+        Channels<VEC> v[kStep];
+        int count = 0;
 #pragma unroll
-      for (int u = 0; u < kStatRows; ++u) {
-        v[u] = numbers_of(raw[u]);
-        count += at.row + r0 + u * at.step < at.rows;
-      }
-      add_rows<VEC, SHARED>(v, count, n, m);
-      if (count > kStep) add_rows<VEC, SHARED>(v + kStep, count - kStep, n, m);
+        for (int u = 0; u < kStep; ++u) {
+          v[u] = Channels<VEC>{};
+          if (at.row + r0 + (first + u) * at.step < at.rows) {
+            v[u] = numbers_of(slot[(first + u) * kNormThreads]);
+            ++count;
+          }
+        }
+        if (count > 0) add_rows<VEC, SHARED>(v, count, n, m);
+      };
+      static_assert(kSlots == 3 * kStep, "three groups are on their way");
+      fetched<2>();
+      take(0);
+      fetched<1>();
+      take(kStep);
+      fetched<0>();
+      take(2 * kStep);
     }
   }
   // parts[y][unit of the tile], and the cells of each in counts[y]
@@ -184,7 +198,7 @@ __global__ void __launch_bounds__(kNormThreads, VEC == 8 ? 2 : 3) norm_graph_ker
   }
   __syncthreads();
   const int lane = threadIdx.x & 31, warp = threadIdx.x / 32;
-  const int32_t groups = group_of(sh, at.tile_channels - 1) + 1, units = SHARED ? a.width / VEC : a.width;
+  const int32_t groups = group_of(plan, at.tile_channels - 1) + 1, units = SHARED ? a.width / VEC : a.width;
   const int32_t lanes = 1 << sh.lanes_log, y0 = lane >> sh.lanes_log, stride = sh.across * kEach;
   for (int32_t g = warp; g < groups; g += kNormThreads / 32) {
     float sum = 0.f, total = 0.f;
@@ -213,18 +227,18 @@ __global__ void __launch_bounds__(kNormThreads, VEC == 8 ? 2 : 3) norm_graph_ker
       if (g == 0) block_cells = make_float2(total, 0.f);  // of any group
     }
   }
-  if (sh.cluster_log > 0) {
+  if (plan.cluster_log > 0) {
     cluster_arrive();
     cluster_wait();
   }
   __syncthreads();
   for (int32_t g = threadIdx.x; g < groups; g += kNormThreads) {
     float2 p = group_parts[g];
-    if (sh.cluster_log > 0) {
+    if (plan.cluster_log > 0) {
       // the blocks' parts, in the order of their ranks
       float cells = 0.f;
       Moments all = {0.f, 0.f};
-      for (int32_t r = 0; r < 1 << sh.cluster_log; ++r) {
+      for (int32_t r = 0; r < 1 << plan.cluster_log; ++r) {
         const float2 o = of_rank(group_parts + g, r);
         join(cells, all, of_rank(&block_cells, r).x, Moments{o.x, o.y});
       }
@@ -235,33 +249,35 @@ __global__ void __launch_bounds__(kNormThreads, VEC == 8 ? 2 : 3) norm_graph_ker
     group_stats[g] = st;
     if (at.rank == 0) a.stats[(int64_t)at.graph * a.groups + at.tile_first / a.width + g] = st;
   }
-  if (sh.cluster_log > 0) cluster_arrive();  // the others' shared memory has been read
+  if (plan.cluster_log > 0) cluster_arrive();  // the others' shared memory has been read
   __syncthreads();
   if (mine) {
     float mean[VEC], rstd[VEC];
 #pragma unroll
     for (int c = 0; c < VEC; ++c) {
       if (c == 0 || !SHARED) {
-        const float2 st = group_stats[group_of(sh, at.channel - at.tile_first + c)];
+        const float2 st = group_stats[group_of(plan, at.channel - at.tile_first + c)];
         mean[c] = st.x, rstd[c] = st.y;
       } else {
         mean[c] = mean[0], rstd[c] = rstd[0];
       }
     }
     for (int32_t r0 = last; r0 >= 0; r0 -= chunk) {
-      if (r0 < last) load(r0);
-#pragma unroll
-      for (int u = 0; u < kStatRows; ++u) {
+      if (r0 < last) {
+        load(r0);
+        fetched<0>();
+      }
+#pragma unroll 4
+      for (int u = 0; u < kSlots; ++u) {
         if (at.row + r0 + u * at.step >= at.rows) break;
-        Channels<VEC> v = numbers_of(raw[u]);
+        Channels<VEC> v = numbers_of(slot[u * kNormThreads]);
 #pragma unroll
         for (int k = 0; k < VEC; ++k) v.v[k] = activated<ACT>(fmaf((v.v[k] - mean[k]) * rstd[k], w[k], b[k]));
         store_channels<Y, VEC>(y + (int64_t)(r0 + u * at.step) * a.F, v);
       }
     }
   }
-  if (sh.cluster_log > 0) cluster_wait();
-  graph_kernel_ends();
+  if (plan.cluster_log > 0) cluster_wait();
 }
 
 // stats of a group from its pieces' moments, in 64 bits; `units` moments of `cells` channels each for a group.  A block, or
@@ -366,13 +382,14 @@ template <typename X, typename Y, int ACT>
 dg_status_t forward(const Graph* g, const NormArgs& a, dg_type_t x, dg_type_t y, cudaStream_t s) {
   const int vec = norm_vector(a, x, y);
   const bool shared = vec > 1 && a.width % vec == 0;
-  if (const GraphPlan plan = graph_plan(g, a, vec, sizeof(X), kStatRows, shared); plan.graphs > 0) {
+  if (const GraphPlan plan = graph_plan(g, a, vec, sizeof(X), kSlots, shared); plan.blocks > 0) {
     DG_CUDA((by_vector<sizeof(X) == 2 && sizeof(Y) == 2>(vec, [&](auto v) {
       constexpr int VEC = decltype(v)::value;
-      return shared ? launch_graphs(plan, norm_graph_kernel<X, Y, ACT, VEC, true>, s, a)
-                    : launch_graphs(plan, norm_graph_kernel<X, Y, ACT, VEC, false>, s, a);
+      constexpr size_t kBytes = (size_t)kSlots * kNormThreads * VEC * sizeof(X);
+      return shared ? launch_graphs(plan, norm_graph_kernel<X, Y, ACT, VEC, true>, kBytes, s, a)
+                    : launch_graphs(plan, norm_graph_kernel<X, Y, ACT, VEC, false>, kBytes, s, a);
     })));
-    count_launches((plan.long_graphs > 0) + (plan.graphs > plan.long_graphs));
+    count_launches(1);
     return DG_OK;
   }
   const NormShape sh = norm_shape(g, a, vec);
@@ -430,17 +447,17 @@ int norm_vector(const NormArgs& a, dg_type_t x, dg_type_t y) {
 }
 
 GraphPlan graph_plan(const Graph* g, const NormArgs& a, int vec, int x_bytes, int rows_kept, bool shared) {
-  // bytes of a graph in a tile: up to kShort one block takes them, up to kLong a cluster
-  constexpr int64_t kShort = 256 << 10, kLong = 1 << 20;
-  GraphPlan plan{};
+  GraphPlan plan{}, none{};
   const int64_t longest = g->batch_longest < 0 ? g->n : g->batch_longest;
   const int32_t vectors = a.F / vec;
   // the fewest vectors that whole groups fill
   int32_t least = a.width;
   while (least % vec) least += a.width;
   least /= vec;
-  if (least > kNormThreads) return plan;
-  auto shape = [&](int32_t across, int cluster_log) {
+  if (least > kNormThreads) return none;
+  plan.by_width = 1.f / a.width;
+  plan.order = g->batch_order;
+  auto shape = [&](int32_t across) {
     GraphShape sh{};
     sh.vec = vec;
     const int32_t parts = vectors / least, tiles = (vectors + across - 1) / across;  // of even width
@@ -448,40 +465,49 @@ GraphPlan graph_plan(const Graph* g, const NormArgs& a, int vec, int x_bytes, in
     sh.by_across = (65536 + sh.across - 1) / sh.across;
     sh.down = kNormThreads / sh.across;
     sh.tiles = (vectors + sh.across - 1) / sh.across;
-    sh.cluster_log = cluster_log;
     const int32_t units = shared ? a.width / vec : a.width;
     while (sh.lanes_log < 5 && (1 << sh.lanes_log) < units) ++sh.lanes_log;
-    sh.by_width = 1.f / a.width;
-    sh.order = g->batch_order;
     return sh;
   };
-  // Long graphs: lines of 128 bytes, or sectors of 32 where the graphs are few; their rows are spread over a cluster.
   auto narrow = [&](int bytes) {
     int32_t across = least;
     while (across * vec * x_bytes < bytes && across + least <= vectors && across + least <= kNormThreads) across += least;
     return across;
   };
+  auto kept = [&](const GraphShape& sh) { return (int64_t)sh.down * rows_kept; };  // rows in a block's shared memory
+  // Few graphs: clusters, in tiles of whole lines, or of sectors where that leaves SMs without a block.
   int32_t across = narrow(128);
   if (a.graphs * (vectors / across) < g->sm_count) across = narrow(32);
-  plan.shape[0] = shape(across, kClusterLog);
-  if (plan.shape[0].tiles > 65535 || longest * plan.shape[0].across * vec * x_bytes > kLong) return plan;
-  if (a.graphs << kClusterLog >= (int64_t)1 << 31) return plan;
-  plan.graphs = a.graphs;
-  plan.long_graphs = 1;
-  if (!g->batch_lengths) return plan;
-  // The others: as wide as leaves an average graph four registerfuls of a block at most.  2048 graphs of 1 to 2500 rows of
-  // 128: TIME
-  auto fits = [&](int32_t wide) { return 4 * (int64_t)(kNormThreads / wide) * rows_kept * a.graphs >= a.rows; };
-  while (across + least <= vectors && across + least <= kNormThreads && fits(across + least)) across += least;
-  plan.shape[1] = shape(across, 0);
-  const int64_t most = kShort / ((int64_t)plan.shape[1].across * vec * x_bytes);
-  int64_t lo = 0, hi = a.graphs;
-  while (lo < hi) {
-    const int64_t mid = (lo + hi) / 2;
-    if (g->batch_lengths[mid] > most) lo = mid + 1; else hi = mid;
+  GraphShape& first = plan.shape[0];
+  first = shape(across);
+  if (a.graphs * first.tiles < 2 * (int64_t)g->sm_count) {
+    if (longest > (kept(first) << kClusterLog) * 2) return none;
+    plan.cluster_log = kClusterLog;
+    plan.long_graphs = (int32_t)a.graphs;
+    plan.blocks = plan.long_blocks = (int32_t)(a.graphs * first.tiles << kClusterLog);
+    return plan;
   }
-  plan.long_graphs = lo;
-  plan.shape[1].first = (int32_t)lo;
+  // Many: those of more than two times what a block keeps in narrow tiles, the others as wide as an average graph leaves
+  // threads with rows.  2048 graphs of 1 to 2500 rows of 128: TIME
+  first = shape(narrow(64));
+  if (longest > 8 * kept(first)) return none;
+  across = first.across;
+  while (across + least <= vectors && across + least <= kNormThreads &&
+         2 * (int64_t)(kNormThreads / (across + least)) * rows_kept * a.graphs >= a.rows)
+    across += least;
+  plan.shape[1] = shape(across);
+  if (g->batch_lengths) {
+    const int64_t most = 2 * kept(plan.shape[1]);
+    int64_t lo = 0, hi = a.graphs;
+    while (lo < hi) {
+      const int64_t mid = (lo + hi) / 2;
+      if (g->batch_lengths[mid] > most) lo = mid + 1; else hi = mid;
+    }
+    plan.long_graphs = (int32_t)lo;
+  }
+  plan.blocks = plan.long_graphs * (int64_t)first.tiles + (a.graphs - plan.long_graphs) * plan.shape[1].tiles;
+  if (plan.blocks >= (int64_t)1 << 31) return none;
+  plan.long_blocks = plan.long_graphs * first.tiles;
   return plan;
 }
 

@@ -153,18 +153,12 @@ __device__ __forceinline__ void store_channels(T* p, const Channels<VEC>& r) {
   }
 }
 
-// The same as it is stored: what waits in registers for the second use.
+// VEC numbers as they are stored, from shared memory.
 template <typename T, int VEC>
 struct RawChannels {
   std::conditional_t<sizeof(T) * VEC == 16, uint4,
                      std::conditional_t<sizeof(T) * VEC == 8, uint2, std::conditional_t<sizeof(T) * VEC == 4, uint32_t, uint16_t>>> v;
 };
-template <typename T, int VEC>
-__device__ __forceinline__ RawChannels<T, VEC> load_raw(const T* p) {
-  RawChannels<T, VEC> r;
-  r.v = *reinterpret_cast<const decltype(r.v)*>(p);
-  return r;
-}
 template <typename T, int VEC>
 __device__ __forceinline__ Channels<VEC> numbers_of(const RawChannels<T, VEC>& q) {
   uint32_t w[4] = {};
@@ -183,6 +177,26 @@ __device__ __forceinline__ Channels<VEC> numbers_of(const RawChannels<T, VEC>& q
       r.v[c] = __uint_as_float(c % 2 ? w[c / 2] & 0xffff0000u : w[c / 2] << 16);
   }
   return r;
+}
+// Copies a vector into the thread's own place in shared memory, behind its back where the hardware copies that many bytes.
+template <typename T, int VEC>
+__device__ __forceinline__ void fetch(RawChannels<T, VEC>* to, const T* from) {
+  constexpr int kBytes = sizeof(T) * VEC;
+  if constexpr (kBytes >= 4) {
+    const uint32_t at = (uint32_t)__cvta_generic_to_shared(to);
+    if constexpr (kBytes == 16)
+      asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(at), "l"(from) : "memory");
+    else
+      asm volatile("cp.async.ca.shared.global [%0], [%1], %2;" ::"r"(at), "l"(from), "n"(kBytes) : "memory");
+  } else {
+    to->v = *reinterpret_cast<const uint16_t*>(from);
+  }
+}
+__device__ __forceinline__ void fetch_group() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+// All but the latest PENDING groups have arrived.
+template <int PENDING>
+__device__ __forceinline__ void fetched() {
+  asm volatile("cp.async.wait_group %0;" ::"n"(PENDING) : "memory");
 }
 
 // A thread's channels: what does not change along its rows.
@@ -270,22 +284,24 @@ __device__ __forceinline__ double block_sum(double v) {
 // ---- a cluster of blocks for a graph and a tile of channels: short graphs -------------------------------------------
 
 // A cluster of blocks takes the rows of one graph in the channels of a tile, which holds whole groups: what it sums it
-// needs nowhere else, and rows that fit its registers are read once.
+// needs nowhere else.  Every thread fetches its rows into places of its own in shared memory, all at once, and rows that fit
+// there are read once.
 constexpr int kClusterLog = 3;
 constexpr int kTileGroups = 128;  // most groups of a tile
 struct GraphShape {
   int32_t vec, across, down, tiles;
   uint32_t by_across;    // thread / across = thread * by_across >> 16
-  int32_t cluster_log;   // log2 of the blocks
   int32_t lanes_log;     // log2 of the threads along a group's units, at most 5
-  float by_width;        // 1 / width: groups of a tile's channels
-  int32_t first;         // place in `order` of the launch's first graph
-  const int32_t* order;  // graphs, longest first; null: one graph
 };
-// A call's two launches: long graphs, then the others.
+// One launch: long graphs in narrow tiles first, then the others in wide ones; or, where the graphs are few, all of them in
+// narrow ones by clusters.
 struct GraphPlan {
-  GraphShape shape[2];
-  int64_t long_graphs, graphs;  // 0 graphs: not a call for these kernels
+  GraphShape shape[2];     // of long graphs, of the others
+  const int32_t* order;    // graphs, longest first; null: one graph
+  int64_t blocks;          // 0: not a call for these kernels
+  int32_t long_blocks, long_graphs;
+  int32_t cluster_log;     // log2 of the blocks of a cluster
+  float by_width;          // 1 / width: groups of a tile's channels
 };
 GraphPlan graph_plan(const Graph* g, const NormArgs& a, int vec, int x_bytes, int rows_kept, bool shared);
 
@@ -298,26 +314,27 @@ struct GraphPlace {
   int32_t rows;
   int64_t base;                    // of that row's first channel, in numbers
 };
-__device__ __forceinline__ GraphPlace graph_place(const NormArgs& a, const GraphShape& sh) {
+__device__ __forceinline__ GraphPlace graph_place(const NormArgs& a, const GraphPlan& plan, const GraphShape& sh, bool is_long) {
   GraphPlace r;
-  const int32_t at = sh.first + (blockIdx.x >> sh.cluster_log);
-  r.rank = blockIdx.x & ((1 << sh.cluster_log) - 1);
-  r.graph = sh.order ? sh.order[at] : 0;
+  const uint32_t item = (is_long ? blockIdx.x : blockIdx.x - plan.long_blocks) >> plan.cluster_log;
+  r.rank = blockIdx.x & ((1 << plan.cluster_log) - 1);
+  const int32_t at = item / (uint32_t)sh.tiles, tile = item - at * sh.tiles;
+  r.graph = plan.order ? plan.order[is_long ? at : at + plan.long_graphs] : 0;
   const Rows rows = rows_of(a, r.graph);
   r.rows = (int32_t)(rows.hi - rows.lo);
-  r.tile_first = blockIdx.y * sh.across * sh.vec;
+  r.tile_first = tile * sh.across * sh.vec;
   r.tile_channels = min(sh.across * sh.vec, a.F - r.tile_first);
   r.y = threadIdx.x * sh.by_across >> 16;
   r.x = threadIdx.x - r.y * sh.across;
   r.channel = r.y < sh.down && r.x * sh.vec < r.tile_channels ? r.tile_first + r.x * sh.vec : a.F;
   r.row = r.rank * sh.down + r.y;
-  r.step = sh.down << sh.cluster_log;
+  r.step = sh.down << plan.cluster_log;
   r.base = (rows.lo + r.row) * a.F + r.channel;
   return r;
 }
 // The group of a channel of the tile: at most 2048 channels, so that the product is off by less than 1 / (2 width).
-__device__ __forceinline__ int32_t group_of(const GraphShape& sh, int32_t channel) {
-  return (int32_t)((channel + 0.5f) * sh.by_width);
+__device__ __forceinline__ int32_t group_of(const GraphPlan& plan, int32_t channel) {
+  return (int32_t)((channel + 0.5f) * plan.by_width);
 }
 __device__ __forceinline__ void cluster_arrive() { asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory"); }
 __device__ __forceinline__ void cluster_wait() { asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory"); }
@@ -335,37 +352,22 @@ __device__ __forceinline__ float warp_total(float v) {
   for (int o = 16; o > 0; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
   return v;
 }
-// The launch of the other graphs may begin once all blocks of this one have; it ends behind it, by its last block.
-__device__ __forceinline__ void graph_kernel_begins() { cudaTriggerProgrammaticLaunchCompletion(); }
-__device__ __forceinline__ void graph_kernel_ends() {
-  if (blockIdx.x == gridDim.x - 1 && blockIdx.y == gridDim.y - 1) cudaGridDependencySynchronize();
-}
-
-// Both launches of a plan.
 template <typename... P, typename... A>
-cudaError_t launch_graphs(const GraphPlan& plan, void (*kernel)(NormArgs, GraphShape, P...), cudaStream_t s, const NormArgs& a,
-                          const A&... args) {
-  const int64_t counts[2] = {plan.long_graphs, plan.graphs - plan.long_graphs};
-  bool before = false;
-  for (int i = 0; i < 2; ++i) {
-    if (counts[i] == 0) continue;
-    const GraphShape& sh = plan.shape[i];
-    cudaLaunchAttribute attributes[2] = {};
-    attributes[0].id = cudaLaunchAttributeClusterDimension;
-    attributes[0].val.clusterDim.x = 1u << sh.cluster_log;
-    attributes[0].val.clusterDim.y = attributes[0].val.clusterDim.z = 1;
-    attributes[1].id = cudaLaunchAttributeProgrammaticStreamSerialization;
-    attributes[1].val.programmaticStreamSerializationAllowed = 1;
-    cudaLaunchConfig_t config{};
-    config.gridDim = dim3((unsigned)(counts[i] << sh.cluster_log), (unsigned)sh.tiles);
-    config.blockDim = dim3(kNormThreads);
-    config.stream = s;
-    config.attrs = attributes;
-    config.numAttrs = before ? 2 : 1;
-    if (cudaError_t e = cudaLaunchKernelEx(&config, kernel, a, sh, args...)) return e;
-    before = true;
-  }
-  return cudaSuccess;
+cudaError_t launch_graphs(const GraphPlan& plan, void (*kernel)(NormArgs, GraphPlan, P...), size_t shared, cudaStream_t s,
+                          const NormArgs& a, const A&... args) {
+  if (cudaError_t e = cudaFuncSetAttribute((const void*)kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)shared)) return e;
+  cudaLaunchAttribute attribute{};
+  attribute.id = cudaLaunchAttributeClusterDimension;
+  attribute.val.clusterDim.x = 1u << plan.cluster_log;
+  attribute.val.clusterDim.y = attribute.val.clusterDim.z = 1;
+  cudaLaunchConfig_t config{};
+  config.gridDim = dim3((unsigned)plan.blocks);
+  config.blockDim = dim3(kNormThreads);
+  config.dynamicSmemBytes = shared;
+  config.stream = s;
+  config.attrs = &attribute;
+  config.numAttrs = plan.cluster_log > 0 ? 1 : 0;
+  return cudaLaunchKernelEx(&config, kernel, a, plan, args...);
 }
 
 // ---- one block for a group, where a call has no scratch ---------------------------------------------------------

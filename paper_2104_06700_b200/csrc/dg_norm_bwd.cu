@@ -7,7 +7,8 @@
 namespace dg {
 namespace {
 
-constexpr int kRows = 4;  // in flight per thread, of each matrix
+constexpr int kRows = 4;   // in flight per thread, of each matrix
+constexpr int kSlots = 8;  // rows of a thread in shared memory, in two groups: three blocks on an SM
 
 // partial[piece][channel] = (sum of d, sum of d hat).  The sums of every kRows rows are added to the thread's.
 template <typename X, typename Y, int ACT, int VEC>
@@ -153,12 +154,13 @@ __global__ void __launch_bounds__(kJoinThreads)
 // Short graphs: sums, A and B and the results in one launch.  graph_sums[graph][channel] = (sum of d, sum of d hat), or, for
 // one graph, the gradients themselves.
 template <typename X, typename Y, int ACT, int VEC>
-__global__ void __launch_bounds__(kNormThreads, VEC == 8 ? 1 : 2)
-    norm_graph_bwd_kernel(NormArgs a, GraphShape sh, float2* graph_sums, float* dweight, float* dbias) {
+__global__ void __launch_bounds__(kNormThreads, VEC == 8 ? 2 : 3)
+    norm_graph_bwd_kernel(const __grid_constant__ NormArgs a, const __grid_constant__ GraphPlan plan, float2* graph_sums, float* dweight, float* dbias) {
   __shared__ float2 parts[kNormThreads * VEC], group_sums[kTileGroups], group_means[kTileGroups];
-  graph_kernel_begins();
-  const GraphPlace at = graph_place(a, sh);
-  const int32_t chunk = at.step * kRows, first_group = at.tile_first / a.width;
+  const bool is_long = blockIdx.x < plan.long_blocks;
+  const GraphShape sh = is_long ? plan.shape[0] : plan.shape[1];
+  const GraphPlace at = graph_place(a, plan, sh, is_long);
+  const int32_t chunk = at.step * kSlots, first_group = at.tile_first / a.width;
   const X* x = static_cast<const X*>(a.X) + at.base;
   const Y* dy = static_cast<const Y*>(a.dY) + at.base;
   X* dx = static_cast<X*>(a.out) + at.base;
@@ -168,22 +170,24 @@ __global__ void __launch_bounds__(kNormThreads, VEC == 8 ? 1 : 2)
   if (mine) {
 #pragma unroll
     for (int k = 0; k < VEC; ++k) {
-      group[k] = group_of(sh, at.channel - at.tile_first + k);
+      group[k] = group_of(plan, at.channel - at.tile_first + k);
       const float2 st = a.stats[(int64_t)at.graph * a.groups + first_group + group[k]];
       f.mean[k] = st.x, f.rstd[k] = st.y;
       f.w[k] = a.weight ? a.weight[at.channel + k] : 1.f;
       f.b[k] = a.bias ? a.bias[at.channel + k] : 0.f;
     }
   }
-  RawChannels<X, VEC> v[kRows];
-  RawChannels<Y, VEC> d[kRows];
+  extern __shared__ uint4 slots[];
+  RawChannels<X, VEC>* const v = reinterpret_cast<RawChannels<X, VEC>*>(slots) + threadIdx.x;
+  RawChannels<Y, VEC>* const d = reinterpret_cast<RawChannels<Y, VEC>*>(reinterpret_cast<RawChannels<X, VEC>*>(slots) + kSlots * kNormThreads) + threadIdx.x;
   auto load = [&](int32_t r0) {
 #pragma unroll
-    for (int u = 0; u < kRows; ++u) {
+    for (int u = 0; u < kSlots; ++u) {
       if (at.row + r0 + u * at.step < at.rows) {
-        v[u] = load_raw<X, VEC>(x + (int64_t)(r0 + u * at.step) * a.F);
-        d[u] = load_raw<Y, VEC>(dy + (int64_t)(r0 + u * at.step) * a.F);
+        fetch<X, VEC>(v + u * kNormThreads, x + (int64_t)(r0 + u * at.step) * a.F);
+        fetch<Y, VEC>(d + u * kNormThreads, dy + (int64_t)(r0 + u * at.step) * a.F);
       }
+      if (u % kRows == kRows - 1) fetch_group();
     }
   };
   float2 total[VEC] = {};
@@ -192,23 +196,30 @@ __global__ void __launch_bounds__(kNormThreads, VEC == 8 ? 1 : 2)
     for (int32_t r0 = 0; at.row + r0 < at.rows; r0 += chunk) {
       last = r0;
       load(r0);
-      float2 s[VEC] = {};
+      auto take = [&](int first) {
+        float2 s[VEC] = {};
 #pragma unroll
-      for (int u = 0; u < kRows; ++u) {
-        if (at.row + r0 + u * at.step >= at.rows) break;
-        const Channels<VEC> vx = numbers_of(v[u]), vd = numbers_of(d[u]);
+        for (int u = first; u < first + kRows; ++u) {
+          if (at.row + r0 + u * at.step >= at.rows) break;
+          const Channels<VEC> vx = numbers_of(v[u * kNormThreads]), vd = numbers_of(d[u * kNormThreads]);
+#pragma unroll
+          for (int k = 0; k < VEC; ++k) {
+            const float q = before_activation<ACT>(vd.v[k], vx.v[k], f.mean[k], f.rstd[k], f.w[k], f.b[k]);
+            s[k].x += q;
+            s[k].y = fmaf(q, (vx.v[k] - f.mean[k]) * f.rstd[k], s[k].y);
+          }
+        }
 #pragma unroll
         for (int k = 0; k < VEC; ++k) {
-          const float q = before_activation<ACT>(vd.v[k], vx.v[k], f.mean[k], f.rstd[k], f.w[k], f.b[k]);
-          s[k].x += q;
-          s[k].y = fmaf(q, (vx.v[k] - f.mean[k]) * f.rstd[k], s[k].y);
+          total[k].x += s[k].x;
+          total[k].y += s[k].y;
         }
-      }
-#pragma unroll
-      for (int k = 0; k < VEC; ++k) {
-        total[k].x += s[k].x;
-        total[k].y += s[k].y;
-      }
+      };
+      static_assert(kSlots == 2 * kRows, "two groups are on their way");
+      fetched<1>();
+      take(0);
+      fetched<0>();
+      take(kRows);
     }
   }
   // parts[y][channel of the tile]
@@ -229,7 +240,7 @@ __global__ void __launch_bounds__(kNormThreads, VEC == 8 ? 1 : 2)
   }
   __syncthreads();
   const int lane = threadIdx.x & 31, warp = threadIdx.x / 32;
-  const int32_t groups = group_of(sh, at.tile_channels - 1) + 1, lanes = 1 << sh.lanes_log;
+  const int32_t groups = group_of(plan, at.tile_channels - 1) + 1, lanes = 1 << sh.lanes_log;
   // several groups a warp: `lanes` threads along the channels of each
   for (int32_t g0 = warp * (32 >> sh.lanes_log); g0 < groups; g0 += (kNormThreads / 32) * (32 >> sh.lanes_log)) {
     const int32_t g = g0 + (lane >> sh.lanes_log);
@@ -248,7 +259,7 @@ __global__ void __launch_bounds__(kNormThreads, VEC == 8 ? 1 : 2)
     }
     if (g < groups && (lane & (lanes - 1)) == 0) group_sums[g] = make_float2(s1, s2);
   }
-  const int32_t cluster = 1 << sh.cluster_log;
+  const int32_t cluster = 1 << plan.cluster_log;
   if (cluster > 1) {
     cluster_arrive();
     cluster_wait();
@@ -294,11 +305,14 @@ __global__ void __launch_bounds__(kNormThreads, VEC == 8 ? 1 : 2)
       A[k] = m.x, B[k] = m.y;
     }
     for (int32_t r0 = last; r0 >= 0; r0 -= chunk) {
-      if (r0 < last) load(r0);
-#pragma unroll
-      for (int u = 0; u < kRows; ++u) {
+      if (r0 < last) {
+        load(r0);
+        fetched<0>();
+      }
+#pragma unroll 2
+      for (int u = 0; u < kSlots; ++u) {
         if (at.row + r0 + u * at.step >= at.rows) break;
-        const Channels<VEC> vx = numbers_of(v[u]), vd = numbers_of(d[u]);
+        const Channels<VEC> vx = numbers_of(v[u * kNormThreads]), vd = numbers_of(d[u * kNormThreads]);
         Channels<VEC> r;
 #pragma unroll
         for (int k = 0; k < VEC; ++k) {
@@ -311,7 +325,6 @@ __global__ void __launch_bounds__(kNormThreads, VEC == 8 ? 1 : 2)
     }
   }
   if (cluster > 1) cluster_wait();
-  graph_kernel_ends();
 }
 
 template <typename X, typename Y, int ACT, int VEC>
@@ -431,25 +444,27 @@ dg_status_t backward(const Graph* g, const NormArgs& a, dg_type_t x, dg_type_t y
   const int vec = norm_vector(a, x, y);
   const unsigned weight_blocks = (unsigned)((a.F + 7) / 8);
   void* memory = nullptr;
-  const GraphPlan plan = graph_plan(g, a, vec, sizeof(X), kRows, false);
-  const size_t graph_bytes = weights && plan.graphs > 1 ? (size_t)plan.graphs * a.F * sizeof(float2) : 0;
-  if (plan.graphs > 0 && (!graph_bytes || scratch_alloc(g, graph_bytes, s, &memory) == cudaSuccess)) {
+  const GraphPlan plan = graph_plan(g, a, vec, sizeof(X), kSlots, false);
+  const size_t graph_bytes = weights && a.graphs > 1 ? (size_t)a.graphs * a.F * sizeof(float2) : 0;
+  if (plan.blocks > 0 && (!graph_bytes || scratch_alloc(g, graph_bytes, s, &memory) == cudaSuccess)) {
     float2* sums = static_cast<float2*>(memory);
     cudaError_t e = by_vector<kWide>(vec, [&](auto v) {
-      return launch_graphs(plan, norm_graph_bwd_kernel<X, Y, ACT, decltype(v)::value>, s, a, sums, dweight, dbias);
+      constexpr int VEC = decltype(v)::value;
+      constexpr size_t kBytes = (size_t)kSlots * kNormThreads * VEC * (sizeof(X) + sizeof(Y));
+      return launch_graphs(plan, norm_graph_bwd_kernel<X, Y, ACT, VEC>, kBytes, s, a, sums, dweight, dbias);
     });
     if (e == cudaSuccess && sums)
-      e = launch_kernel(norm_weight_sums_kernel, dim3(weight_blocks), kJoinThreads, s, true, a.F, (const float2*)sums, plan.graphs,
+      e = launch_kernel(norm_weight_sums_kernel, dim3(weight_blocks), kJoinThreads, s, true, a.F, (const float2*)sums, a.graphs,
                         dweight, dbias);
     pool_free(memory, s);
     DG_CUDA(e);
-    count_launches((plan.long_graphs > 0) + (plan.graphs > plan.long_graphs) + (sums != nullptr));
+    count_launches(1 + (sums != nullptr));
     return DG_OK;
   }
   const NormShape sh = norm_shape(g, a, vec);
   const size_t partial_bytes = (size_t)sh.pieces * a.F * sizeof(float2);
   const int64_t pairs = a.out ? a.graphs * a.groups : 0;
-  if (plan.graphs > 0 || scratch_alloc(g, partial_bytes + (size_t)pairs * sizeof(float2), s, &memory) != cudaSuccess) {
+  if (plan.blocks > 0 || scratch_alloc(g, partial_bytes + (size_t)pairs * sizeof(float2), s, &memory) != cudaSuccess) {
     int across = 1;
     while (across < a.width && across < kNormThreads) across *= 2;
     if (weights)
