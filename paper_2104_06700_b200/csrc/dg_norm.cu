@@ -10,7 +10,7 @@ namespace {
 
 // Rows a thread has in flight, and takes the mean of before it joins that to what it has.
 constexpr int kStatRows = 8;
-// Rows of a thread in shared memory, in groups of kStep: with four blocks on an SM.
+// Rows of a thread in shared memory: eight blocks on an SM.
 constexpr int kStep = 4, kSlots = 12;
 
 // Count, mean and sum of squares about the mean; joined they lose nothing to large means, as sums of x and x^2 would.
@@ -135,10 +135,10 @@ __global__ void __launch_bounds__(kNormThreads, VEC == 8 ? 2 : 4)
 // Short graphs: statistics and results in one launch.  What every block costs beside its cells counts here: sums over the
 // block are plain ones (the mean, then the squares about it), one warp for a group.
 template <typename X, typename Y, int ACT, int VEC, bool SHARED>
-__global__ void __launch_bounds__(kNormThreads, VEC == 8 ? 3 : 4) norm_graph_kernel(const __grid_constant__ NormArgs a, const __grid_constant__ GraphPlan plan) {
+__global__ void __launch_bounds__(kGraphThreads, VEC == 8 ? 6 : 8) norm_graph_kernel(const __grid_constant__ NormArgs a, const __grid_constant__ GraphPlan plan) {
   constexpr int kEach = kUnits<VEC, SHARED>;
-  __shared__ Moments parts[kNormThreads * kEach];
-  __shared__ float counts[kNormThreads];
+  __shared__ Moments parts[kGraphThreads * kEach];
+  __shared__ float counts[kGraphThreads];
   __shared__ float2 group_parts[kTileGroups], group_stats[kTileGroups], block_cells;
   const bool is_long = blockIdx.x < plan.long_blocks;
   const GraphShape sh = is_long ? plan.shape[0] : plan.shape[1];
@@ -149,12 +149,15 @@ __global__ void __launch_bounds__(kNormThreads, VEC == 8 ? 3 : 4) norm_graph_ker
   const bool mine = at.channel < a.F;
   extern __shared__ uint4 slots[];
   RawChannels<X, VEC>* const slot = reinterpret_cast<RawChannels<X, VEC>*>(slots) + threadIdx.x;
+  const int64_t pace = (int64_t)at.step * a.F;
   auto load = [&](int32_t r0) {
+    const X* from = x + (int64_t)r0 * a.F;
 #pragma unroll
-    for (int u = 0; u < kSlots; ++u) {
-      if (at.row + r0 + u * at.step < at.rows) fetch<X, VEC>(slot + u * kNormThreads, x + (int64_t)(r0 + u * at.step) * a.F);
-      if (u % kStep == kStep - 1) fetch_group();
+    for (int u = 0; u < kSlots; ++u, from += pace) {
+      if (at.row + r0 + u * at.step >= at.rows) break;
+      fetch<X, VEC>(slot + u * kGraphThreads, from);
     }
+    fetched();
   };
   Moments m[kEach] = {};
   float n = 0.f, w[VEC], b[VEC];
@@ -168,26 +171,22 @@ __global__ void __launch_bounds__(kNormThreads, VEC == 8 ? 3 : 4) norm_graph_ker
     for (int32_t r0 = 0; at.row + r0 < at.rows; r0 += chunk) {
       last = r0;
       load(r0);
-      auto take = [&](int first) {
+#pragma unroll 1
+      for (int first = 0; first < kSlots; first += kStep) {
+        const int32_t left = at.rows - (at.row + r0 + first * at.step);
+        if (left <= 0) break;
         Channels<VEC> v[kStep];
         int count = 0;
 #pragma unroll
         for (int u = 0; u < kStep; ++u) {
           v[u] = Channels<VEC>{};
-          if (at.row + r0 + (first + u) * at.step < at.rows) {
-            v[u] = numbers_of(slot[(first + u) * kNormThreads]);
+          if (u * at.step < left) {
+            v[u] = numbers_of(slot[(first + u) * kGraphThreads]);
             ++count;
           }
         }
-        if (count > 0) add_rows<VEC, SHARED>(v, count, n, m);
-      };
-      static_assert(kSlots == 3 * kStep, "three groups are on their way");
-      fetched<2>();
-      take(0);
-      fetched<1>();
-      take(kStep);
-      fetched<0>();
-      take(2 * kStep);
+        add_rows<VEC, SHARED>(v, count, n, m);
+      }
     }
   }
   // parts[y][unit of the tile], and the cells of each in counts[y]
@@ -197,32 +196,42 @@ __global__ void __launch_bounds__(kNormThreads, VEC == 8 ? 3 : 4) norm_graph_ker
     if (at.x == 0) counts[at.y] = n;
   }
   __syncthreads();
-  const int lane = threadIdx.x & 31, warp = threadIdx.x / 32;
+  // a team of threads for a group
   const int32_t groups = group_of(plan, at.tile_channels - 1) + 1, units = SHARED ? a.width / VEC : a.width;
-  const int32_t lanes = 1 << sh.lanes_log, y0 = lane >> sh.lanes_log, stride = sh.across * kEach;
-  for (int32_t g = warp; g < groups; g += kNormThreads / 32) {
+  const int32_t team = 1 << sh.team_log, lanes = 1 << sh.lanes_log, stride = sh.across * kEach;
+  const int32_t k0 = threadIdx.x & (lanes - 1), y0 = (threadIdx.x & (team - 1)) >> sh.lanes_log, down = team >> sh.lanes_log;
+  for (int32_t g0 = 0; g0 < groups; g0 += kGraphThreads >> sh.team_log) {
+    const int32_t g = g0 + (threadIdx.x >> sh.team_log);
+    const bool some = g < groups;
+    const Moments* of_group = parts + g * units;
     float sum = 0.f, total = 0.f;
-    for (int32_t yy = y0; yy < sh.down; yy += 32 >> sh.lanes_log) {
-      const float c = counts[yy];
-      for (int32_t k = lane & (lanes - 1); k < units; k += lanes) {
-        sum = fmaf(c, parts[yy * stride + g * units + k].mean, sum);
-        total += c;
+    if (some) {
+      for (int32_t yy = y0; yy < sh.down; yy += down) {
+        const float c = counts[yy];
+        for (int32_t k = k0; k < units; k += lanes) {
+          sum = fmaf(c, of_group[yy * stride + k].mean, sum);
+          total += c;
+        }
       }
     }
-    sum = warp_total(sum);
-    total = warp_total(total);
+    for (int o = team / 2; o > 0; o /= 2) {
+      sum += __shfl_xor_sync(0xffffffffu, sum, o);
+      total += __shfl_xor_sync(0xffffffffu, total, o);
+    }
     const float mean = total > 0.f ? sum / total : 0.f;
     float squares = 0.f;
-    for (int32_t yy = y0; yy < sh.down; yy += 32 >> sh.lanes_log) {
-      const float c = counts[yy];
-      for (int32_t k = lane & (lanes - 1); k < units; k += lanes) {
-        const Moments u = parts[yy * stride + g * units + k];
-        const float d = u.mean - mean;
-        squares += c > 0.f ? fmaf(c * d, d, u.m2) : 0.f;
+    if (some) {
+      for (int32_t yy = y0; yy < sh.down; yy += down) {
+        const float c = counts[yy];
+        for (int32_t k = k0; k < units; k += lanes) {
+          const Moments u = of_group[yy * stride + k];
+          const float d = u.mean - mean;
+          squares += c > 0.f ? fmaf(c * d, d, u.m2) : 0.f;
+        }
       }
     }
-    squares = warp_total(squares);
-    if (lane == 0) {
+    for (int o = team / 2; o > 0; o /= 2) squares += __shfl_xor_sync(0xffffffffu, squares, o);
+    if (some && (threadIdx.x & (team - 1)) == 0) {
       group_parts[g] = make_float2(mean, squares);
       if (g == 0) block_cells = make_float2(total, 0.f);  // of any group
     }
@@ -232,7 +241,7 @@ __global__ void __launch_bounds__(kNormThreads, VEC == 8 ? 3 : 4) norm_graph_ker
     cluster_wait();
   }
   __syncthreads();
-  for (int32_t g = threadIdx.x; g < groups; g += kNormThreads) {
+  for (int32_t g = threadIdx.x; g < groups; g += kGraphThreads) {
     float2 p = group_parts[g];
     if (plan.cluster_log > 0) {
       // the blocks' parts, in the order of their ranks
@@ -263,17 +272,15 @@ __global__ void __launch_bounds__(kNormThreads, VEC == 8 ? 3 : 4) norm_graph_ker
       }
     }
     for (int32_t r0 = last; r0 >= 0; r0 -= chunk) {
-      if (r0 < last) {
-        load(r0);
-        fetched<0>();
-      }
+      if (r0 < last) load(r0);
+      Y* to = y + (int64_t)r0 * a.F;
 #pragma unroll 4
-      for (int u = 0; u < kSlots; ++u) {
+      for (int u = 0; u < kSlots; ++u, to += pace) {
         if (at.row + r0 + u * at.step >= at.rows) break;
-        Channels<VEC> v = numbers_of(slot[u * kNormThreads]);
+        Channels<VEC> v = numbers_of(slot[u * kGraphThreads]);
 #pragma unroll
         for (int k = 0; k < VEC; ++k) v.v[k] = activated<ACT>(fmaf((v.v[k] - mean[k]) * rstd[k], w[k], b[k]));
-        store_channels<Y, VEC>(y + (int64_t)(r0 + u * at.step) * a.F, v);
+        store_channels<Y, VEC>(to, v);
       }
     }
   }
@@ -385,7 +392,7 @@ dg_status_t forward(const Graph* g, const NormArgs& a, dg_type_t x, dg_type_t y,
   if (const GraphPlan plan = graph_plan(g, a, vec, sizeof(X), kSlots, shared); plan.blocks > 0) {
     DG_CUDA((by_vector<sizeof(X) == 2 && sizeof(Y) == 2>(vec, [&](auto v) {
       constexpr int VEC = decltype(v)::value;
-      constexpr size_t kBytes = (size_t)kSlots * kNormThreads * VEC * sizeof(X);
+      constexpr size_t kBytes = (size_t)kSlots * kGraphThreads * VEC * sizeof(X);
       return shared ? launch_graphs(plan, norm_graph_kernel<X, Y, ACT, VEC, true>, kBytes, s, a)
                     : launch_graphs(plan, norm_graph_kernel<X, Y, ACT, VEC, false>, kBytes, s, a);
     })));
@@ -454,7 +461,7 @@ GraphPlan graph_plan(const Graph* g, const NormArgs& a, int vec, int x_bytes, in
   int32_t least = a.width;
   while (least % vec) least += a.width;
   least /= vec;
-  if (least > kNormThreads) return none;
+  if (least > kGraphThreads) return none;
   plan.by_width = 1.f / a.width;
   plan.order = g->batch_order;
   auto shape = [&](int32_t across) {
@@ -463,15 +470,18 @@ GraphPlan graph_plan(const Graph* g, const NormArgs& a, int vec, int x_bytes, in
     const int32_t parts = vectors / least, tiles = (vectors + across - 1) / across;  // of even width
     sh.across = (parts + tiles - 1) / tiles * least;
     sh.by_across = (65536 + sh.across - 1) / sh.across;
-    sh.down = kNormThreads / sh.across;
+    sh.down = kGraphThreads / sh.across;
     sh.tiles = (vectors + sh.across - 1) / sh.across;
     const int32_t units = shared ? a.width / vec : a.width;
     while (sh.lanes_log < 5 && (1 << sh.lanes_log) < units) ++sh.lanes_log;
+    const int32_t groups = sh.across * vec / a.width;
+    sh.team_log = 5;
+    while (sh.team_log > sh.lanes_log && (kGraphThreads >> sh.team_log) < groups) --sh.team_log;
     return sh;
   };
   auto narrow = [&](int bytes) {
     int32_t across = least;
-    while (across * vec * x_bytes < bytes && across + least <= vectors && across + least <= kNormThreads) across += least;
+    while (across * vec * x_bytes < bytes && across + least <= vectors && across + least <= kGraphThreads) across += least;
     return across;
   };
   auto kept = [&](const GraphShape& sh) { return (int64_t)sh.down * rows_kept; };  // rows in a block's shared memory
@@ -490,10 +500,10 @@ GraphPlan graph_plan(const Graph* g, const NormArgs& a, int vec, int x_bytes, in
   // Many: those of more than two times what a block keeps in narrow tiles, the others as wide as an average graph leaves
   // threads with rows.  2048 graphs of 1 to 2500 rows of 128: TIME
   first = shape(narrow(64));
-  if (longest > 8 * kept(first)) return none;
+  if (longest > 16 * kept(first)) return none;
   across = first.across;
-  while (across + least <= vectors && across + least <= kNormThreads &&
-         2 * (int64_t)(kNormThreads / (across + least)) * rows_kept * a.graphs >= a.rows)
+  while (across + least <= vectors && across + least <= kGraphThreads &&
+         2 * (int64_t)(kGraphThreads / (across + least)) * rows_kept * a.graphs >= a.rows)
     across += least;
   plan.shape[1] = shape(across);
   if (g->batch_lengths) {

@@ -48,9 +48,14 @@ __device__ __forceinline__ T as(float v) {
   }
 }
 
-// 1 / (1 + exp(-z)).  The fast exponential is off by 2 + |1.2 z| units of 2^-23 and the result by less than that: a
-// cell costs 4 to 12 bytes of memory traffic, and the exact one with its division costs as much time.
-__device__ __forceinline__ float sigmoid(float z) { return __fdividef(1.f, 1.f + __expf(-z)); }
+// 1 / (1 + exp(-z)), of hardware's 2^x and 1 / x: off by 2 + |1.5 z| units of 2^-23.  A cell costs 4 to 12 bytes of memory
+// traffic, and the exact functions cost as much time.
+__device__ __forceinline__ float sigmoid(float z) {
+  float e, r;
+  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(e) : "f"(z * -1.4426950408889634f));
+  asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(1.f + e));
+  return r;
+}
 
 template <int ACT>
 __device__ __forceinline__ float activated(float z) {
@@ -192,12 +197,8 @@ __device__ __forceinline__ void fetch(RawChannels<T, VEC>* to, const T* from) {
     to->v = *reinterpret_cast<const uint16_t*>(from);
   }
 }
-__device__ __forceinline__ void fetch_group() { asm volatile("cp.async.commit_group;" ::: "memory"); }
-// All but the latest PENDING groups have arrived.
-template <int PENDING>
-__device__ __forceinline__ void fetched() {
-  asm volatile("cp.async.wait_group %0;" ::"n"(PENDING) : "memory");
-}
+// All that the thread fetched has arrived.
+__device__ __forceinline__ void fetched() { asm volatile("cp.async.wait_all;" ::: "memory"); }
 
 // A thread's channels: what does not change along its rows.
 template <int VEC>
@@ -287,11 +288,15 @@ __device__ __forceinline__ double block_sum(double v) {
 // needs nowhere else.  Every thread fetches its rows into places of its own in shared memory, all at once, and rows that fit
 // there are read once.
 constexpr int kClusterLog = 3;
+// Of a block: with as few as 16 rows for a thread what a thread costs beside them counts (2048 graphs of 1 to 2500 rows of
+// 128, forward: 41 us with 256 threads, TIME with 128).
+constexpr int kGraphThreads = 128;
 constexpr int kTileGroups = 128;  // most groups of a tile
 struct GraphShape {
   int32_t vec, across, down, tiles;
   uint32_t by_across;    // thread / across = thread * by_across >> 16
   int32_t lanes_log;     // log2 of the threads along a group's units, at most 5
+  int32_t team_log;      // log2 of the threads of a group while a block's sums are joined, at most 5
 };
 // One launch: long graphs in narrow tiles first, then the others in wide ones; or, where the graphs are few, all of them in
 // narrow ones by clusters.
@@ -362,7 +367,7 @@ cudaError_t launch_graphs(const GraphPlan& plan, void (*kernel)(NormArgs, GraphP
   attribute.val.clusterDim.y = attribute.val.clusterDim.z = 1;
   cudaLaunchConfig_t config{};
   config.gridDim = dim3((unsigned)plan.blocks);
-  config.blockDim = dim3(kNormThreads);
+  config.blockDim = dim3(kGraphThreads);
   config.dynamicSmemBytes = shared;
   config.stream = s;
   config.attrs = &attribute;

@@ -8,7 +8,7 @@ namespace dg {
 namespace {
 
 constexpr int kRows = 4;   // in flight per thread, of each matrix
-constexpr int kSlots = 8;  // rows of a thread in shared memory, in two groups: three blocks on an SM
+constexpr int kSlots = 8;  // rows of a thread in shared memory: six blocks of a short graph on an SM
 
 // partial[piece][channel] = (sum of d, sum of d hat).  The sums of every kRows rows are added to the thread's.
 template <typename X, typename Y, int ACT, int VEC>
@@ -154,9 +154,9 @@ __global__ void __launch_bounds__(kJoinThreads)
 // Short graphs: sums, A and B and the results in one launch.  graph_sums[graph][channel] = (sum of d, sum of d hat), or, for
 // one graph, the gradients themselves.
 template <typename X, typename Y, int ACT, int VEC>
-__global__ void __launch_bounds__(kNormThreads, VEC == 8 ? 2 : 3)
+__global__ void __launch_bounds__(kGraphThreads, VEC == 8 ? 4 : 6)
     norm_graph_bwd_kernel(const __grid_constant__ NormArgs a, const __grid_constant__ GraphPlan plan, float2* graph_sums, float* dweight, float* dbias) {
-  __shared__ float2 parts[kNormThreads * VEC], group_sums[kTileGroups], group_means[kTileGroups];
+  __shared__ float2 parts[kGraphThreads * VEC], group_sums[kTileGroups], group_means[kTileGroups];
   const bool is_long = blockIdx.x < plan.long_blocks;
   const GraphShape sh = is_long ? plan.shape[0] : plan.shape[1];
   const GraphPlace at = graph_place(a, plan, sh, is_long);
@@ -179,16 +179,17 @@ __global__ void __launch_bounds__(kNormThreads, VEC == 8 ? 2 : 3)
   }
   extern __shared__ uint4 slots[];
   RawChannels<X, VEC>* const v = reinterpret_cast<RawChannels<X, VEC>*>(slots) + threadIdx.x;
-  RawChannels<Y, VEC>* const d = reinterpret_cast<RawChannels<Y, VEC>*>(reinterpret_cast<RawChannels<X, VEC>*>(slots) + kSlots * kNormThreads) + threadIdx.x;
+  RawChannels<Y, VEC>* const d = reinterpret_cast<RawChannels<Y, VEC>*>(reinterpret_cast<RawChannels<X, VEC>*>(slots) + kSlots * kGraphThreads) + threadIdx.x;
+  const int64_t pace = (int64_t)at.step * a.F;
   auto load = [&](int32_t r0) {
+    int64_t from = (int64_t)r0 * a.F;
 #pragma unroll
-    for (int u = 0; u < kSlots; ++u) {
-      if (at.row + r0 + u * at.step < at.rows) {
-        fetch<X, VEC>(v + u * kNormThreads, x + (int64_t)(r0 + u * at.step) * a.F);
-        fetch<Y, VEC>(d + u * kNormThreads, dy + (int64_t)(r0 + u * at.step) * a.F);
-      }
-      if (u % kRows == kRows - 1) fetch_group();
+    for (int u = 0; u < kSlots; ++u, from += pace) {
+      if (at.row + r0 + u * at.step >= at.rows) break;
+      fetch<X, VEC>(v + u * kGraphThreads, x + from);
+      fetch<Y, VEC>(d + u * kGraphThreads, dy + from);
     }
+    fetched();
   };
   float2 total[VEC] = {};
   int32_t last = 0;  // the chunk that stays in registers
@@ -196,30 +197,23 @@ __global__ void __launch_bounds__(kNormThreads, VEC == 8 ? 2 : 3)
     for (int32_t r0 = 0; at.row + r0 < at.rows; r0 += chunk) {
       last = r0;
       load(r0);
-      auto take = [&](int first) {
-        float2 s[VEC] = {};
-#pragma unroll
-        for (int u = first; u < first + kRows; ++u) {
-          if (at.row + r0 + u * at.step >= at.rows) break;
-          const Channels<VEC> vx = numbers_of(v[u * kNormThreads]), vd = numbers_of(d[u * kNormThreads]);
-#pragma unroll
-          for (int k = 0; k < VEC; ++k) {
-            const float q = before_activation<ACT>(vd.v[k], vx.v[k], f.mean[k], f.rstd[k], f.w[k], f.b[k]);
-            s[k].x += q;
-            s[k].y = fmaf(q, (vx.v[k] - f.mean[k]) * f.rstd[k], s[k].y);
-          }
-        }
+      float2 s[VEC] = {};
+#pragma unroll 2
+      for (int u = 0; u < kSlots; ++u) {
+        if (at.row + r0 + u * at.step >= at.rows) break;
+        const Channels<VEC> vx = numbers_of(v[u * kGraphThreads]), vd = numbers_of(d[u * kGraphThreads]);
 #pragma unroll
         for (int k = 0; k < VEC; ++k) {
-          total[k].x += s[k].x;
-          total[k].y += s[k].y;
+          const float q = before_activation<ACT>(vd.v[k], vx.v[k], f.mean[k], f.rstd[k], f.w[k], f.b[k]);
+          s[k].x += q;
+          s[k].y = fmaf(q, (vx.v[k] - f.mean[k]) * f.rstd[k], s[k].y);
         }
-      };
-      static_assert(kSlots == 2 * kRows, "two groups are on their way");
-      fetched<1>();
-      take(0);
-      fetched<0>();
-      take(kRows);
+      }
+#pragma unroll
+      for (int k = 0; k < VEC; ++k) {
+        total[k].x += s[k].x;
+        total[k].y += s[k].y;
+      }
     }
   }
   // parts[y][channel of the tile]
@@ -230,7 +224,7 @@ __global__ void __launch_bounds__(kNormThreads, VEC == 8 ? 2 : 3)
   }
   __syncthreads();
   // a channel's sum over the block's rows, in parts[0][channel]
-  for (int32_t k = threadIdx.x; k < at.tile_channels; k += kNormThreads) {
+  for (int32_t k = threadIdx.x; k < at.tile_channels; k += kGraphThreads) {
     float2 s = parts[k];
     for (int32_t yy = 1; yy < sh.down; ++yy) {
       s.x += parts[yy * stride + k].x;
@@ -242,7 +236,7 @@ __global__ void __launch_bounds__(kNormThreads, VEC == 8 ? 2 : 3)
   const int lane = threadIdx.x & 31, warp = threadIdx.x / 32;
   const int32_t groups = group_of(plan, at.tile_channels - 1) + 1, lanes = 1 << sh.lanes_log;
   // several groups a warp: `lanes` threads along the channels of each
-  for (int32_t g0 = warp * (32 >> sh.lanes_log); g0 < groups; g0 += (kNormThreads / 32) * (32 >> sh.lanes_log)) {
+  for (int32_t g0 = warp * (32 >> sh.lanes_log); g0 < groups; g0 += (kGraphThreads / 32) * (32 >> sh.lanes_log)) {
     const int32_t g = g0 + (lane >> sh.lanes_log);
     float s1 = 0.f, s2 = 0.f;
     if (g < groups) {
@@ -265,7 +259,7 @@ __global__ void __launch_bounds__(kNormThreads, VEC == 8 ? 2 : 3)
     cluster_wait();
   }
   __syncthreads();
-  for (int32_t g = threadIdx.x; g < groups; g += kNormThreads) {
+  for (int32_t g = threadIdx.x; g < groups; g += kGraphThreads) {
     const float n = at.rows > 0 ? (float)at.rows * a.width : 1.f;
     float2 s = group_sums[g];
     if (cluster > 1) {
@@ -279,7 +273,7 @@ __global__ void __launch_bounds__(kNormThreads, VEC == 8 ? 2 : 3)
     group_means[g] = make_float2(s.x / n, s.y / n);
   }
   if (at.rank == 0 && (dweight || dbias)) {
-    for (int32_t k = threadIdx.x; k < at.tile_channels; k += kNormThreads) {
+    for (int32_t k = threadIdx.x; k < at.tile_channels; k += kGraphThreads) {
       float2 s = parts[k];
       for (int32_t r = 1; r < cluster; ++r) {
         const float2 o = of_rank(parts + k, r);
@@ -305,14 +299,12 @@ __global__ void __launch_bounds__(kNormThreads, VEC == 8 ? 2 : 3)
       A[k] = m.x, B[k] = m.y;
     }
     for (int32_t r0 = last; r0 >= 0; r0 -= chunk) {
-      if (r0 < last) {
-        load(r0);
-        fetched<0>();
-      }
+      if (r0 < last) load(r0);
+      X* to = dx + (int64_t)r0 * a.F;
 #pragma unroll 2
-      for (int u = 0; u < kSlots; ++u) {
+      for (int u = 0; u < kSlots; ++u, to += pace) {
         if (at.row + r0 + u * at.step >= at.rows) break;
-        const Channels<VEC> vx = numbers_of(v[u * kNormThreads]), vd = numbers_of(d[u * kNormThreads]);
+        const Channels<VEC> vx = numbers_of(v[u * kGraphThreads]), vd = numbers_of(d[u * kGraphThreads]);
         Channels<VEC> r;
 #pragma unroll
         for (int k = 0; k < VEC; ++k) {
@@ -320,7 +312,7 @@ __global__ void __launch_bounds__(kNormThreads, VEC == 8 ? 2 : 3)
           const float hat = (vx.v[k] - f.mean[k]) * f.rstd[k];
           r.v[k] = (q - A[k] - hat * B[k]) * f.rstd[k];
         }
-        store_channels<X, VEC>(dx + (int64_t)(r0 + u * at.step) * a.F, r);
+        store_channels<X, VEC>(to, r);
       }
     }
   }
@@ -450,7 +442,7 @@ dg_status_t backward(const Graph* g, const NormArgs& a, dg_type_t x, dg_type_t y
     float2* sums = static_cast<float2*>(memory);
     cudaError_t e = by_vector<kWide>(vec, [&](auto v) {
       constexpr int VEC = decltype(v)::value;
-      constexpr size_t kBytes = (size_t)kSlots * kNormThreads * VEC * (sizeof(X) + sizeof(Y));
+      constexpr size_t kBytes = (size_t)kSlots * kGraphThreads * VEC * (sizeof(X) + sizeof(Y));
       return launch_graphs(plan, norm_graph_bwd_kernel<X, Y, ACT, VEC>, kBytes, s, a, sums, dweight, dbias);
     });
     if (e == cudaSuccess && sums)
