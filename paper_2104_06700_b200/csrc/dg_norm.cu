@@ -11,7 +11,7 @@ namespace {
 // Rows a thread has in flight, and takes the mean of before it joins that to what it has.
 constexpr int kStatRows = 8;
 // Rows of a thread in shared memory: eight blocks on an SM.
-constexpr int kStep = 4, kSlots = 12;
+constexpr int kStep = 4, kRing = 3, kSlots = kStep * kRing;
 
 // Count, mean and sum of squares about the mean; joined they lose nothing to large means, as sums of x and x^2 would.
 struct Moments {
@@ -143,52 +143,40 @@ __global__ void __launch_bounds__(kGraphThreads, VEC == 8 ? 6 : 8) norm_graph_ke
   const bool is_long = blockIdx.x < plan.long_blocks;
   const GraphShape sh = is_long ? plan.shape[0] : plan.shape[1];
   const GraphPlace at = graph_place(a, plan, sh, is_long);
-  const int32_t chunk = at.step * kSlots;
   const X* x = static_cast<const X*>(a.X) + at.base;
   Y* y = static_cast<Y*>(a.out) + at.base;
   const bool mine = at.channel < a.F;
   extern __shared__ uint4 slots[];
   RawChannels<X, VEC>* const slot = reinterpret_cast<RawChannels<X, VEC>*>(slots) + threadIdx.x;
   const int64_t pace = (int64_t)at.step * a.F;
-  auto load = [&](int32_t r0) {
-    const X* from = x + (int64_t)r0 * a.F;
+  // the thread's rows, and in groups of kStep
+  const int32_t count = mine && at.row < at.rows ? (at.rows - at.row + at.step - 1) / at.step : 0;
+  const int32_t steps = (count + kStep - 1) / kStep;
+  auto fetch_rows = [&](int32_t q, int place) {
+    const X* from = x + q * kStep * pace;
 #pragma unroll
-    for (int u = 0; u < kSlots; ++u, from += pace) {
-      if (at.row + r0 + u * at.step >= at.rows) break;
-      fetch<X, VEC>(slot + u * kGraphThreads, from);
-    }
-    fetched();
+    for (int u = 0; u < kStep; ++u, from += pace)
+      if (q * kStep + u < count) fetch<X, VEC>(slot + (place * kStep + u) * kGraphThreads, from);
   };
   Moments m[kEach] = {};
   float n = 0.f, w[VEC], b[VEC];
-  int32_t last = 0;  // the chunk that stays in registers
   if (mine) {
 #pragma unroll
     for (int c = 0; c < VEC; ++c) {
       w[c] = a.weight ? a.weight[at.channel + c] : 1.f;
       b[c] = a.bias ? a.bias[at.channel + c] : 0.f;
     }
-    for (int32_t r0 = 0; at.row + r0 < at.rows; r0 += chunk) {
-      last = r0;
-      load(r0);
-#pragma unroll 1
-      for (int first = 0; first < kSlots; first += kStep) {
-        const int32_t left = at.rows - (at.row + r0 + first * at.step);
-        if (left <= 0) break;
-        Channels<VEC> v[kStep];
-        int count = 0;
-#pragma unroll
-        for (int u = 0; u < kStep; ++u) {
-          v[u] = Channels<VEC>{};
-          if (u * at.step < left) {
-            v[u] = numbers_of(slot[(first + u) * kGraphThreads]);
-            ++count;
-          }
-        }
-        add_rows<VEC, SHARED>(v, count, n, m);
-      }
-    }
   }
+  ring_forward<kRing>(steps, fetch_rows, [&](int32_t q, int place) {
+    Channels<VEC> v[kStep];
+    const int32_t rows = min(count - q * kStep, kStep);
+#pragma unroll
+    for (int u = 0; u < kStep; ++u) {
+      v[u] = Channels<VEC>{};
+      if (u < rows) v[u] = numbers_of(slot[(place * kStep + u) * kGraphThreads]);
+    }
+    add_rows<VEC, SHARED>(v, rows, n, m);
+  });
   // parts[y][unit of the tile], and the cells of each in counts[y]
   if (at.y < sh.down) {
 #pragma unroll
@@ -271,18 +259,17 @@ __global__ void __launch_bounds__(kGraphThreads, VEC == 8 ? 6 : 8) norm_graph_ke
         mean[c] = mean[0], rstd[c] = rstd[0];
       }
     }
-    for (int32_t r0 = last; r0 >= 0; r0 -= chunk) {
-      if (r0 < last) load(r0);
-      Y* to = y + (int64_t)r0 * a.F;
-#pragma unroll 4
-      for (int u = 0; u < kSlots; ++u, to += pace) {
-        if (at.row + r0 + u * at.step >= at.rows) break;
-        Channels<VEC> v = numbers_of(slot[u * kGraphThreads]);
+    ring_back<kRing>(steps, fetch_rows, [&](int32_t q, int place) {
+      Y* to = y + q * kStep * pace;
+#pragma unroll
+      for (int u = 0; u < kStep; ++u, to += pace) {
+        if (q * kStep + u >= count) break;
+        Channels<VEC> v = numbers_of(slot[(place * kStep + u) * kGraphThreads]);
 #pragma unroll
         for (int k = 0; k < VEC; ++k) v.v[k] = activated<ACT>(fmaf((v.v[k] - mean[k]) * rstd[k], w[k], b[k]));
         store_channels<Y, VEC>(to, v);
       }
-    }
+    });
   }
   if (plan.cluster_log > 0) cluster_wait();
 }

@@ -197,8 +197,45 @@ __device__ __forceinline__ void fetch(RawChannels<T, VEC>* to, const T* from) {
     to->v = *reinterpret_cast<const uint16_t*>(from);
   }
 }
-// All that the thread fetched has arrived.
-__device__ __forceinline__ void fetched() { asm volatile("cp.async.wait_all;" ::: "memory"); }
+__device__ __forceinline__ void fetch_group() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+// All but the latest PENDING groups have arrived.
+template <int PENDING>
+__device__ __forceinline__ void fetched() {
+  asm volatile("cp.async.wait_group %0;" ::"n"(PENDING) : "memory");
+}
+
+// A thread's rows, in groups of STEP, through a ring of RING groups of places in shared memory.  `fetch_rows(group, place)` begins
+// the copies of a group (of those of its rows that exist), `use(group, place)` takes it from there; the places of a group are
+// filled again when it has been used.  Forward: the last groups stay where they are.  Back: those first, then the others.
+template <int RING, typename Fetch, typename Use>
+__device__ __forceinline__ void ring_forward(int32_t groups, Fetch fetch_rows, Use use) {
+#pragma unroll
+  for (int q = 0; q < RING; ++q) {
+    if (q < groups) fetch_rows(q, q);
+    fetch_group();
+  }
+  int place = 0;
+#pragma unroll 1
+  for (int32_t q = 0; q < groups; ++q) {
+    fetched<RING - 1>();
+    use(q, place);
+    if (q + RING < groups) fetch_rows(q + RING, place);
+    fetch_group();
+    place = place + 1 == RING ? 0 : place + 1;
+  }
+}
+template <int RING, typename Fetch, typename Use>
+__device__ __forceinline__ void ring_back(int32_t groups, Fetch fetch_rows, Use use) {
+  int place = (groups - 1) % RING;  // of the last group
+#pragma unroll 1
+  for (int32_t q = groups - 1; q >= 0; --q) {
+    fetched<RING - 1>();  // the last RING groups arrived long ago
+    use(q, place);
+    if (q >= RING) fetch_rows(q - RING, place);
+    fetch_group();
+    place = place == 0 ? RING - 1 : place - 1;
+  }
+}
 
 // A thread's channels: what does not change along its rows.
 template <int VEC>

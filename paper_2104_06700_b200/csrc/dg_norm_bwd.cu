@@ -8,7 +8,8 @@ namespace dg {
 namespace {
 
 constexpr int kRows = 4;   // in flight per thread, of each matrix
-constexpr int kSlots = 8;  // rows of a thread in shared memory: six blocks of a short graph on an SM
+// Rows of a thread in shared memory: six blocks of short graphs on an SM.
+constexpr int kStep = 2, kRing = 4, kSlots = kStep * kRing;
 
 // partial[piece][channel] = (sum of d, sum of d hat).  The sums of every kRows rows are added to the thread's.
 template <typename X, typename Y, int ACT, int VEC>
@@ -160,7 +161,7 @@ __global__ void __launch_bounds__(kGraphThreads, VEC == 8 ? 4 : 6)
   const bool is_long = blockIdx.x < plan.long_blocks;
   const GraphShape sh = is_long ? plan.shape[0] : plan.shape[1];
   const GraphPlace at = graph_place(a, plan, sh, is_long);
-  const int32_t chunk = at.step * kSlots, first_group = at.tile_first / a.width;
+  const int32_t first_group = at.tile_first / a.width;
   const X* x = static_cast<const X*>(a.X) + at.base;
   const Y* dy = static_cast<const Y*>(a.dY) + at.base;
   X* dx = static_cast<X*>(a.out) + at.base;
@@ -181,41 +182,33 @@ __global__ void __launch_bounds__(kGraphThreads, VEC == 8 ? 4 : 6)
   RawChannels<X, VEC>* const v = reinterpret_cast<RawChannels<X, VEC>*>(slots) + threadIdx.x;
   RawChannels<Y, VEC>* const d = reinterpret_cast<RawChannels<Y, VEC>*>(reinterpret_cast<RawChannels<X, VEC>*>(slots) + kSlots * kGraphThreads) + threadIdx.x;
   const int64_t pace = (int64_t)at.step * a.F;
-  auto load = [&](int32_t r0) {
-    int64_t from = (int64_t)r0 * a.F;
+  // the thread's rows, and in groups of kStep
+  const int32_t count = mine && at.row < at.rows ? (at.rows - at.row + at.step - 1) / at.step : 0;
+  const int32_t steps = (count + kStep - 1) / kStep;
+  auto fetch_rows = [&](int32_t q, int place) {
+    int64_t from = q * kStep * pace;
 #pragma unroll
-    for (int u = 0; u < kSlots; ++u, from += pace) {
-      if (at.row + r0 + u * at.step >= at.rows) break;
-      fetch<X, VEC>(v + u * kGraphThreads, x + from);
-      fetch<Y, VEC>(d + u * kGraphThreads, dy + from);
+    for (int u = 0; u < kStep; ++u, from += pace) {
+      if (q * kStep + u >= count) break;
+      fetch<X, VEC>(v + (place * kStep + u) * kGraphThreads, x + from);
+      fetch<Y, VEC>(d + (place * kStep + u) * kGraphThreads, dy + from);
     }
-    fetched();
   };
   float2 total[VEC] = {};
-  int32_t last = 0;  // the chunk that stays in registers
-  if (mine) {
-    for (int32_t r0 = 0; at.row + r0 < at.rows; r0 += chunk) {
-      last = r0;
-      load(r0);
-      float2 s[VEC] = {};
-#pragma unroll 2
-      for (int u = 0; u < kSlots; ++u) {
-        if (at.row + r0 + u * at.step >= at.rows) break;
-        const Channels<VEC> vx = numbers_of(v[u * kGraphThreads]), vd = numbers_of(d[u * kGraphThreads]);
+  ring_forward<kRing>(steps, fetch_rows, [&](int32_t q, int place) {
 #pragma unroll
-        for (int k = 0; k < VEC; ++k) {
-          const float q = before_activation<ACT>(vd.v[k], vx.v[k], f.mean[k], f.rstd[k], f.w[k], f.b[k]);
-          s[k].x += q;
-          s[k].y = fmaf(q, (vx.v[k] - f.mean[k]) * f.rstd[k], s[k].y);
-        }
-      }
+    for (int u = 0; u < kStep; ++u) {
+      if (q * kStep + u >= count) break;
+      const int at_slot = (place * kStep + u) * kGraphThreads;
+      const Channels<VEC> vx = numbers_of(v[at_slot]), vd = numbers_of(d[at_slot]);
 #pragma unroll
       for (int k = 0; k < VEC; ++k) {
-        total[k].x += s[k].x;
-        total[k].y += s[k].y;
+        const float q = before_activation<ACT>(vd.v[k], vx.v[k], f.mean[k], f.rstd[k], f.w[k], f.b[k]);
+        total[k].x += q;
+        total[k].y = fmaf(q, (vx.v[k] - f.mean[k]) * f.rstd[k], total[k].y);
       }
     }
-  }
+  });
   // parts[y][channel of the tile]
   const int32_t stride = sh.across * VEC;
   if (at.y < sh.down) {
@@ -298,13 +291,13 @@ __global__ void __launch_bounds__(kGraphThreads, VEC == 8 ? 4 : 6)
       const float2 m = group_means[group[k]];
       A[k] = m.x, B[k] = m.y;
     }
-    for (int32_t r0 = last; r0 >= 0; r0 -= chunk) {
-      if (r0 < last) load(r0);
-      X* to = dx + (int64_t)r0 * a.F;
-#pragma unroll 2
-      for (int u = 0; u < kSlots; ++u, to += pace) {
-        if (at.row + r0 + u * at.step >= at.rows) break;
-        const Channels<VEC> vx = numbers_of(v[u * kGraphThreads]), vd = numbers_of(d[u * kGraphThreads]);
+    ring_back<kRing>(steps, fetch_rows, [&](int32_t q, int place) {
+      X* to = dx + q * kStep * pace;
+#pragma unroll
+      for (int u = 0; u < kStep; ++u, to += pace) {
+        if (q * kStep + u >= count) break;
+        const int at_slot = (place * kStep + u) * kGraphThreads;
+        const Channels<VEC> vx = numbers_of(v[at_slot]), vd = numbers_of(d[at_slot]);
         Channels<VEC> r;
 #pragma unroll
         for (int k = 0; k < VEC; ++k) {
@@ -314,7 +307,7 @@ __global__ void __launch_bounds__(kGraphThreads, VEC == 8 ? 4 : 6)
         }
         store_channels<X, VEC>(to, r);
       }
-    }
+    });
   }
   if (cluster > 1) cluster_wait();
 }
