@@ -29,7 +29,7 @@ def _stale() -> bool:
     t = os.path.getmtime(LIB_PATH)
     deps = _sources() + [os.path.join(CSRC, "dg_internal.cuh"),
                         os.path.join(CSRC, "dg_aggregate_kernels.cuh"), os.path.join(CSRC, "dg_general.cuh"),
-                        os.path.join(CSRC, "dg_norm.cuh"),
+                        os.path.join(CSRC, "dg_norm.cuh"), os.path.join(CSRC, "dg_pairs.cuh"),
                         os.path.join(INCLUDE, "dg.h")]
     return any(os.path.getmtime(d) > t for d in deps)
 

@@ -11,6 +11,7 @@
 #include <type_traits>
 
 #include "dg_internal.cuh"
+#include "dg_pairs.cuh"
 
 namespace dg {
 namespace {
@@ -146,32 +147,6 @@ __device__ __forceinline__ void store_bytes(uint8_t* p, int left, uint32_t v) {
     for (int j = 0; j < 4; ++j)
       if (j < left) p[j] = (uint8_t)(v >> (8 * j));
   }
-}
-
-// Two numbers side by side: one instruction for both.
-struct Two {
-  uint64_t v;
-};
-__device__ __forceinline__ Two two(float a, float b) {
-  Two r;
-  asm("mov.b64 %0, {%1, %2};" : "=l"(r.v) : "f"(a), "f"(b));
-  return r;
-}
-__device__ __forceinline__ Two both(float a) { return two(a, a); }
-__device__ __forceinline__ float2 apart(Two a) {
-  float2 r;
-  asm("mov.b64 {%0, %1}, %2;" : "=f"(r.x), "=f"(r.y) : "l"(a.v));
-  return r;
-}
-__device__ __forceinline__ Two operator*(Two a, Two b) {
-  Two r;
-  asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r.v) : "l"(a.v), "l"(b.v));
-  return r;
-}
-__device__ __forceinline__ Two fma2(Two a, Two b, Two c) {
-  Two r;
-  asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r.v) : "l"(a.v), "l"(b.v), "l"(c.v));
-  return r;
 }
 
 // What two e4m3 codes stand for.

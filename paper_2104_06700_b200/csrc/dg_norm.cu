@@ -95,32 +95,78 @@ __device__ __forceinline__ void join_block(float& n, Moments (&m)[UNITS], Moment
   }
 }
 
-// partial[piece][unit]: the moments of a piece's rows.
+// partial[piece][unit]: the moments of a piece's rows.  A thread sums differences from the mean of its first rows, and their
+// squares: what is lost when its own mean is taken off is of the order of those rows' distance from the others.
 template <typename X, int VEC, bool SHARED>
-__global__ void __launch_bounds__(kNormThreads, VEC == 8 ? 2 : 4)
+__global__ void __launch_bounds__(kNormThreads, VEC == 8 ? 3 : 4)
     norm_stats_kernel(NormArgs a, NormShape sh, const Piece* pieces, float2* partial) {
-  constexpr int kEach = kUnits<VEC, SHARED>;
+  constexpr int kEach = kUnits<VEC, SHARED>, kP = kPairs<VEC>;
   __shared__ Moments parts[kNormThreads * kEach];
   __shared__ float counts[kNormThreads];
   const Place at = place_of(a, sh, pieces, blockIdx.x);
   Moments m[kEach] = {};
   float n = 0.f;
-  if (at.channel < a.F) {
+  if (at.channel < a.F && at.y < at.piece.rows) {
     const X* x = static_cast<const X*>(a.X) + (int64_t)at.piece.row * a.F + at.channel;
-    for (int32_t r0 = at.y; r0 < at.piece.rows; r0 += at.down * kStatRows) {
-      Channels<VEC> v[kStatRows];
-      int rows = 0;
+    const int32_t rows = (at.piece.rows - at.y + at.down - 1) / at.down;
+    const int64_t pace = (int64_t)at.down * a.F;
+    Two from[kP], sum[kP] = {}, squares[kP] = {};
+    x += at.y * a.F;
+    auto add = [&](const Channels<VEC>& v) {
 #pragma unroll
-      for (int u = 0; u < kStatRows; ++u) {
-        const int32_t r = r0 + u * at.down;
-        v[u] = Channels<VEC>{};
-        if (r < at.piece.rows) {
-          v[u] = load_channels<X, VEC>(x + (int64_t)r * a.F);
-          ++rows;
-        }
+      for (int k = 0; k < kP; ++k) {
+        const Two d = pair_of(v, k) - from[k];
+        sum[k] = sum[k] + d;
+        squares[k] = fma2(d, d, squares[k]);
       }
-      add_rows<VEC, SHARED>(v, rows, n, m);
-      if (rows > kStep) add_rows<VEC, SHARED>(v + kStep, rows - kStep, n, m);
+    };
+    {
+      Channels<VEC> mean = {};
+      const int32_t few = min(rows, kStep);
+#pragma unroll
+      for (int u = 0; u < kStep; ++u) {
+        if (u >= few) break;
+        const Channels<VEC> v = load_channels<X, VEC>(x + u * pace);
+#pragma unroll
+        for (int c = 0; c < VEC; ++c) mean.v[c] += v.v[c];
+      }
+      const float inverse = 1.f / few;
+      if constexpr (SHARED) {
+        float all = 0.f;
+#pragma unroll
+        for (int c = 0; c < VEC; ++c) all += mean.v[c];
+#pragma unroll
+        for (int c = 0; c < VEC; ++c) mean.v[c] = all * (1.f / VEC);
+      }
+#pragma unroll
+      for (int k = 0; k < kP; ++k) from[k] = pair_of(mean, k) * both(inverse);
+    }
+    int32_t r = 0;
+    for (; r + kStatRows <= rows; r += kStatRows, x += kStatRows * pace) {
+      Channels<VEC> v[kStatRows];
+#pragma unroll
+      for (int u = 0; u < kStatRows; ++u) v[u] = load_channels<X, VEC>(x + u * pace);
+#pragma unroll
+      for (int u = 0; u < kStatRows; ++u) add(v[u]);
+    }
+    for (; r < rows; ++r, x += pace) add(load_channels<X, VEC>(x));
+    Channels<VEC> s, q, f;
+#pragma unroll
+    for (int k = 0; k < kP; ++k) set_pair(s, k, sum[k]), set_pair(q, k, squares[k]), set_pair(f, k, from[k]);
+    if constexpr (SHARED) {
+      n = (float)rows * VEC;
+      float total = 0.f, all = 0.f;
+#pragma unroll
+      for (int c = 0; c < VEC; ++c) total += s.v[c], all += q.v[c];
+      const float off = total / n, m2 = fmaf(-off, total, all);
+      m[0] = Moments{f.v[0] + off, m2 < 0.f ? 0.f : m2};  // NaN stays NaN
+    } else {
+      n = (float)rows;
+#pragma unroll
+      for (int c = 0; c < VEC; ++c) {
+        const float off = s.v[c] / n, m2 = fmaf(-off, s.v[c], q.v[c]);
+        m[c] = Moments{f.v[c] + off, m2 < 0.f ? 0.f : m2};  // NaN stays NaN
+      }
     }
   }
   join_block<kEach>(n, m, parts, counts, sh.across, sh.down);
@@ -159,14 +205,9 @@ __global__ void __launch_bounds__(kGraphThreads, VEC == 8 ? 6 : 8) norm_graph_ke
       if (q * kStep + u < count) fetch<X, VEC>(slot + (place * kStep + u) * kGraphThreads, from);
   };
   Moments m[kEach] = {};
-  float n = 0.f, w[VEC], b[VEC];
-  if (mine) {
-#pragma unroll
-    for (int c = 0; c < VEC; ++c) {
-      w[c] = a.weight ? a.weight[at.channel + c] : 1.f;
-      b[c] = a.bias ? a.bias[at.channel + c] : 0.f;
-    }
-  }
+  float n = 0.f;
+  Fixed<VEC> f;
+  if (mine) fix_weights<VEC>(f, a, at.channel);
   ring_forward<kRing>(steps, fetch_rows, [&](int32_t q, int place) {
     Channels<VEC> v[kStep];
     const int32_t rows = min(count - q * kStep, kStep);
@@ -249,24 +290,15 @@ __global__ void __launch_bounds__(kGraphThreads, VEC == 8 ? 6 : 8) norm_graph_ke
   if (plan.cluster_log > 0) cluster_arrive();  // the others' shared memory has been read
   __syncthreads();
   if (mine) {
-    float mean[VEC], rstd[VEC];
-#pragma unroll
-    for (int c = 0; c < VEC; ++c) {
-      if (c == 0 || !SHARED) {
-        const float2 st = group_stats[group_of(plan, at.channel - at.tile_first + c)];
-        mean[c] = st.x, rstd[c] = st.y;
-      } else {
-        mean[c] = mean[0], rstd[c] = rstd[0];
-      }
-    }
+    const int32_t first = at.channel - at.tile_first, shared_group = SHARED ? group_of(plan, first) : 0;
+    fix_stats<VEC>(f, [&](int c) { return group_stats[SHARED ? shared_group : group_of(plan, first + c)]; });
     ring_back<kRing>(steps, fetch_rows, [&](int32_t q, int place) {
       Y* to = y + q * kStep * pace;
 #pragma unroll
       for (int u = 0; u < kStep; ++u, to += pace) {
         if (q * kStep + u >= count) break;
         Channels<VEC> v = numbers_of(slot[(place * kStep + u) * kGraphThreads]);
-#pragma unroll
-        for (int k = 0; k < VEC; ++k) v.v[k] = activated<ACT>(fmaf((v.v[k] - mean[k]) * rstd[k], w[k], b[k]));
+        normalise<ACT, VEC>(v, f);
         store_channels<Y, VEC>(to, v);
       }
     });
@@ -307,43 +339,43 @@ __global__ void norm_join_kernel(NormArgs a, NormShape sh, const Piece* pieces, 
     sum += rows * cells * s1;
     squares += s2;
   }
-  sum = PER_WARP ? warp_sum(sum) : block_sum(sum);
-  squares = PER_WARP ? warp_sum(squares) : block_sum(squares);
+  const double2 both_sums = PER_WARP ? make_double2(warp_sum(sum), warp_sum(squares)) : block_sums(sum, squares);
+  sum = both_sums.x;
+  squares = both_sums.y;
   const double off = sum / n, var = squares / n - off * off;
   // from and the moments of no rows are 0; a variance below 0 is one of rounding (NaN stays NaN)
   if (thread == 0)
     a.stats[pair] = make_float2((float)(from + off), (float)(1.0 / sqrt((var < 0.0 ? 0.0 : var) + (double)a.eps)));
 }
 
+// Every block takes the rows of its piece from the last one back: all pieces are read at the same time, and the L2 holds
+// their ends.
 template <typename X, typename Y, int ACT, int VEC>
-__global__ void __launch_bounds__(kNormThreads, VEC == 8 ? 2 : 4) norm_apply_kernel(NormArgs a, NormShape sh, const Piece* pieces) {
+__global__ void __launch_bounds__(kNormThreads, VEC == 8 ? 3 : 4) norm_apply_kernel(NormArgs a, NormShape sh, const Piece* pieces) {
   constexpr int kRows = 4;
   cudaGridDependencySynchronize();
-  const Place at = place_of(a, sh, pieces, gridDim.x - 1 - blockIdx.x);
-  if (at.channel >= a.F) return;
-  float mean[VEC], rstd[VEC], w[VEC], b[VEC];
-#pragma unroll
-  for (int c = 0; c < VEC; ++c) {
-    const float2 st = a.stats[(int64_t)at.piece.graph * a.groups + (at.channel + c) / a.width];
-    mean[c] = st.x, rstd[c] = st.y;
-    w[c] = a.weight ? a.weight[at.channel + c] : 1.f;
-    b[c] = a.bias ? a.bias[at.channel + c] : 0.f;
-  }
-  const int64_t base = (int64_t)at.piece.row * a.F + at.channel;
+  const Place at = place_of(a, sh, pieces, blockIdx.x);
+  if (at.channel >= a.F || at.y >= at.piece.rows) return;
+  const Fixed<VEC> f = fixed_of<VEC>(a, at.piece.graph, at.channel);
+  int32_t rows = (at.piece.rows - at.y + at.down - 1) / at.down;
+  const int64_t pace = (int64_t)at.down * a.F;
+  const int64_t base = ((int64_t)at.piece.row + at.y) * a.F + at.channel + (rows - 1) * pace;
   const X* x = static_cast<const X*>(a.X) + base;
   Y* y = static_cast<Y*>(a.out) + base;
-  for (int32_t r0 = at.y; r0 < at.piece.rows; r0 += at.down * kRows) {
+  for (; rows >= kRows; rows -= kRows, x -= kRows * pace, y -= kRows * pace) {
     Channels<VEC> v[kRows];
 #pragma unroll
-    for (int u = 0; u < kRows; ++u)
-      if (r0 + u * at.down < at.piece.rows) v[u] = load_channels<X, VEC>(x + (int64_t)(r0 + u * at.down) * a.F);
+    for (int u = 0; u < kRows; ++u) v[u] = load_channels<X, VEC>(x - u * pace);
 #pragma unroll
     for (int u = 0; u < kRows; ++u) {
-      if (r0 + u * at.down >= at.piece.rows) break;
-#pragma unroll
-      for (int c = 0; c < VEC; ++c) v[u].v[c] = activated<ACT>(fmaf((v[u].v[c] - mean[c]) * rstd[c], w[c], b[c]));
-      store_channels<Y, VEC>(y + (int64_t)(r0 + u * at.down) * a.F, v[u]);
+      normalise<ACT, VEC>(v[u], f);
+      store_channels<Y, VEC>(y - u * pace, v[u]);
     }
+  }
+  for (; rows > 0; --rows, x -= pace, y -= pace) {
+    Channels<VEC> v = load_channels<X, VEC>(x);
+    normalise<ACT, VEC>(v, f);
+    store_channels<Y, VEC>(y, v);
   }
 }
 

@@ -12,6 +12,7 @@
 #include <type_traits>
 
 #include "dg_internal.cuh"
+#include "dg_pairs.cuh"
 
 namespace dg {
 
@@ -62,6 +63,16 @@ __device__ __forceinline__ float activated(float z) {
   if constexpr (ACT == DG_ACT_RELU) return z <= 0.f ? 0.f : z;  // NaN stays NaN
   if constexpr (ACT == DG_ACT_SILU) return z * sigmoid(z);
   return z;
+}
+__device__ __forceinline__ Two sigmoid(Two z) {
+  const float2 t = apart(z * both(-1.4426950408889634f));
+  float2 e, r;
+  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(e.x) : "f"(t.x));
+  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(e.y) : "f"(t.y));
+  e = apart(two(e.x, e.y) + both(1.f));
+  asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r.x) : "f"(e.x));
+  asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r.y) : "f"(e.y));
+  return two(r.x, r.y);
 }
 
 // dy act'(z).  The ReLU's border is where z changes its sign: near it (|hat w| is about |b| there and z is off by up to
@@ -237,22 +248,90 @@ __device__ __forceinline__ void ring_back(int32_t groups, Fetch fetch_rows, Use 
   }
 }
 
-// A thread's channels: what does not change along its rows.
+// A thread's channels: what does not change along its rows, in pairs (of one channel twice where it has one).
+template <int VEC>
+constexpr int kPairs = (VEC + 1) / 2;
 template <int VEC>
 struct Fixed {
-  float mean[VEC], rstd[VEC], w[VEC], b[VEC];
+  Two mean[kPairs<VEC>], rstd[kPairs<VEC>], w[kPairs<VEC>], b[kPairs<VEC>];
 };
+template <int VEC>
+__device__ __forceinline__ Two pair_of(const Channels<VEC>& v, int k) {
+  return two(v.v[2 * k], v.v[VEC == 1 ? 0 : 2 * k + 1]);
+}
+template <int VEC>
+__device__ __forceinline__ void set_pair(Channels<VEC>& v, int k, Two p) {
+  const float2 q = apart(p);
+  v.v[2 * k] = q.x;
+  if constexpr (VEC > 1) v.v[2 * k + 1] = q.y;
+}
+template <int VEC>
+__device__ __forceinline__ void fix_weights(Fixed<VEC>& f, const NormArgs& a, int32_t channel) {
+  Channels<VEC> w, b;
+#pragma unroll
+  for (int c = 0; c < VEC; ++c) {
+    w.v[c] = a.weight ? a.weight[channel + c] : 1.f;
+    b.v[c] = a.bias ? a.bias[channel + c] : 0.f;
+  }
+#pragma unroll
+  for (int k = 0; k < kPairs<VEC>; ++k) f.w[k] = pair_of(w, k), f.b[k] = pair_of(b, k);
+}
+// stats(c): (mean, rstd) of the vector's channel c
+template <int VEC, typename Stats>
+__device__ __forceinline__ void fix_stats(Fixed<VEC>& f, Stats stats) {
+  Channels<VEC> mean, rstd;
+#pragma unroll
+  for (int c = 0; c < VEC; ++c) {
+    const float2 st = stats(c);
+    mean.v[c] = st.x, rstd.v[c] = st.y;
+  }
+#pragma unroll
+  for (int k = 0; k < kPairs<VEC>; ++k) f.mean[k] = pair_of(mean, k), f.rstd[k] = pair_of(rstd, k);
+}
 template <int VEC>
 __device__ __forceinline__ Fixed<VEC> fixed_of(const NormArgs& a, int32_t graph, int32_t channel) {
   Fixed<VEC> f;
-#pragma unroll
-  for (int c = 0; c < VEC; ++c) {
-    const float2 st = a.stats[(int64_t)graph * a.groups + (channel + c) / a.width];
-    f.mean[c] = st.x, f.rstd[c] = st.y;
-    f.w[c] = a.weight ? a.weight[channel + c] : 1.f;
-    f.b[c] = a.bias ? a.bias[channel + c] : 0.f;
-  }
+  fix_weights<VEC>(f, a, channel);
+  fix_stats<VEC>(f, [&](int c) { return a.stats[(int64_t)graph * a.groups + (channel + c) / a.width]; });
   return f;
+}
+// act(hat w + b)
+template <int ACT, int VEC>
+__device__ __forceinline__ void normalise(Channels<VEC>& v, const Fixed<VEC>& f) {
+#pragma unroll
+  for (int k = 0; k < kPairs<VEC>; ++k) {
+    Two z = fma2((pair_of(v, k) - f.mean[k]) * f.rstd[k], f.w[k], f.b[k]);
+    if constexpr (ACT == DG_ACT_SILU) z = z * sigmoid(z);
+    if constexpr (ACT == DG_ACT_RELU) {
+      const float2 q = apart(z);
+      z = two(activated<ACT>(q.x), activated<ACT>(q.y));
+    }
+    set_pair(v, k, z);
+  }
+}
+// Of a pair of cells: hat, and d = dy act'(z).
+template <int ACT, int VEC>
+__device__ __forceinline__ void backward_terms(Two x, Two dy, const Fixed<VEC>& f, int k, Two* hat, Two* d) {
+  const Two off = x - f.mean[k];
+  *hat = off * f.rstd[k];
+  if constexpr (ACT == DG_ACT_NONE) {
+    *d = dy;
+  } else {
+    const Two z = fma2(*hat, f.w[k], f.b[k]);
+    if constexpr (ACT == DG_ACT_SILU) {
+      const Two s = sigmoid(z);
+      *d = dy * (s * fma2(z, both(1.f) - s, both(1.f)));
+    } else {
+      const float2 zs = apart(z), ds = apart(dy), bs = apart(f.b[k]);
+      float2 r = make_float2(zs.x <= 0.f ? 0.f : ds.x, zs.y <= 0.f ? 0.f : ds.y);
+      if (!(fabsf(zs.x) >= fabsf(bs.x) * 0x1p-20f) || !(fabsf(zs.y) >= fabsf(bs.y) * 0x1p-20f)) {
+        const float2 xs = apart(x), m = apart(f.mean[k]), q = apart(f.rstd[k]), w = apart(f.w[k]);
+        r.x = before_activation<ACT>(ds.x, xs.x, m.x, q.x, w.x, bs.x);
+        r.y = before_activation<ACT>(ds.y, xs.y, m.y, q.y, w.y, bs.y);
+      }
+      *d = two(r.x, r.y);
+    }
+  }
 }
 
 // Where a thread works: its piece, its first channel, its place along the rows.
@@ -307,17 +386,18 @@ __device__ __forceinline__ double warp_sum(double v) {
   for (int o = 16; o > 0; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
   return v;
 }
-// The sum of v over a block of at most 1024 threads, in every thread and always in the same order.
-__device__ __forceinline__ double block_sum(double v) {
-  __shared__ double sums[32];
-  v = warp_sum(v);
+// The sums of a and b over a block of at most 1024 threads, in every thread and always in the same order.
+__device__ __forceinline__ double2 block_sums(double a, double b) {
+  __shared__ double2 sums[32];
+  a = warp_sum(a);
+  b = warp_sum(b);
   __syncthreads();  // the last call's sums have been read
-  if (threadIdx.x % 32 == 0) sums[threadIdx.x / 32] = v;
+  if (threadIdx.x % 32 == 0) sums[threadIdx.x / 32] = make_double2(a, b);
   __syncthreads();
-  v = 0.0;
-  for (int i = 0; i < (int)blockDim.x / 32; ++i) v += sums[i];
-  return v;
+  const double2 part = threadIdx.x % 32 < blockDim.x / 32 ? sums[threadIdx.x % 32] : make_double2(0.0, 0.0);
+  return make_double2(warp_sum(part.x), warp_sum(part.y));
 }
+__device__ __forceinline__ double block_sum(double v) { return block_sums(v, 0.0).x; }
 
 // ---- a cluster of blocks for a graph and a tile of channels: short graphs -------------------------------------------
 

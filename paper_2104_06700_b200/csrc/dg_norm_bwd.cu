@@ -11,42 +11,87 @@ constexpr int kRows = 4;   // in flight per thread, of each matrix
 // Rows of a thread in shared memory: six blocks of short graphs on an SM.
 constexpr int kStep = 2, kRing = 4, kSlots = kStep * kRing;
 
+// A thread's sums of d and of d hat over rows.
+template <int ACT, int VEC>
+struct Sums {
+  Two d[kPairs<VEC>], dh[kPairs<VEC>];
+  __device__ __forceinline__ void add(const Channels<VEC>& x, const Channels<VEC>& dy, const Fixed<VEC>& f) {
+#pragma unroll
+    for (int k = 0; k < kPairs<VEC>; ++k) {
+      Two hat, q;
+      backward_terms<ACT, VEC>(pair_of(x, k), pair_of(dy, k), f, k, &hat, &q);
+      d[k] = d[k] + q;
+      dh[k] = fma2(q, hat, dh[k]);
+    }
+  }
+  __device__ __forceinline__ void add(const Sums& o) {
+#pragma unroll
+    for (int k = 0; k < kPairs<VEC>; ++k) d[k] = d[k] + o.d[k], dh[k] = dh[k] + o.dh[k];
+  }
+  __device__ __forceinline__ void put(float2 (&total)[VEC]) const {
+    Channels<VEC> s, t;
+#pragma unroll
+    for (int k = 0; k < kPairs<VEC>; ++k) set_pair(s, k, d[k]), set_pair(t, k, dh[k]);
+#pragma unroll
+    for (int c = 0; c < VEC; ++c) total[c] = make_float2(s.v[c], t.v[c]);
+  }
+};
+
+// means(c): (A, B) of the vector's channel c
+template <int VEC, typename Means>
+__device__ __forceinline__ void means_of(Two (&A)[kPairs<VEC>], Two (&B)[kPairs<VEC>], Means means) {
+  Channels<VEC> p, q;
+#pragma unroll
+  for (int c = 0; c < VEC; ++c) {
+    const float2 m = means(c);
+    p.v[c] = m.x, q.v[c] = m.y;
+  }
+#pragma unroll
+  for (int k = 0; k < kPairs<VEC>; ++k) A[k] = pair_of(p, k), B[k] = pair_of(q, k);
+}
+
+// dx = rstd (d w - A - hat B) of a vector
+template <int ACT, int VEC>
+__device__ __forceinline__ Channels<VEC> gradient_of(const Channels<VEC>& x, const Channels<VEC>& dy, const Fixed<VEC>& f,
+                                                     const Two (&A)[kPairs<VEC>], const Two (&B)[kPairs<VEC>]) {
+  Channels<VEC> r;
+#pragma unroll
+  for (int k = 0; k < kPairs<VEC>; ++k) {
+    Two hat, q;
+    backward_terms<ACT, VEC>(pair_of(x, k), pair_of(dy, k), f, k, &hat, &q);
+    set_pair(r, k, (fma2(q, f.w[k], both(-1.f) * A[k]) - hat * B[k]) * f.rstd[k]);
+  }
+  return r;
+}
+
 // partial[piece][channel] = (sum of d, sum of d hat).  The sums of every kRows rows are added to the thread's.
 template <typename X, typename Y, int ACT, int VEC>
-__global__ void __launch_bounds__(kNormThreads) norm_sums_kernel(NormArgs a, NormShape sh, const Piece* pieces, float2* partial) {
+__global__ void __launch_bounds__(kNormThreads, VEC == 8 ? 2 : 3)
+    norm_sums_kernel(NormArgs a, NormShape sh, const Piece* pieces, float2* partial) {
   __shared__ float2 parts[kNormThreads * VEC];
   const Place at = place_of(a, sh, pieces, blockIdx.x);
   float2 total[VEC] = {};
-  if (at.channel < a.F) {
+  if (at.channel < a.F && at.y < at.piece.rows) {
     const Fixed<VEC> f = fixed_of<VEC>(a, at.piece.graph, at.channel);
-    const int64_t base = (int64_t)at.piece.row * a.F + at.channel;
+    int32_t rows = (at.piece.rows - at.y + at.down - 1) / at.down;
+    const int64_t pace = (int64_t)at.down * a.F, base = ((int64_t)at.piece.row + at.y) * a.F + at.channel;
     const X* x = static_cast<const X*>(a.X) + base;
     const Y* dy = static_cast<const Y*>(a.dY) + base;
-    for (int32_t r0 = at.y; r0 < at.piece.rows; r0 += at.down * kRows) {
+    Sums<ACT, VEC> all = {};
+    for (; rows >= kRows; rows -= kRows, x += kRows * pace, dy += kRows * pace) {
       Channels<VEC> v[kRows], d[kRows];
 #pragma unroll
       for (int u = 0; u < kRows; ++u) {
-        const int32_t r = r0 + u * at.down;
-        if (r < at.piece.rows) {
-          v[u] = load_channels<X, VEC>(x + (int64_t)r * a.F);
-          d[u] = load_channels<Y, VEC>(dy + (int64_t)r * a.F);
-        }
+        v[u] = load_channels<X, VEC>(x + u * pace);
+        d[u] = load_channels<Y, VEC>(dy + u * pace);
       }
+      Sums<ACT, VEC> some = {};
 #pragma unroll
-      for (int c = 0; c < VEC; ++c) {
-        float s1 = 0.f, s2 = 0.f;
-#pragma unroll
-        for (int u = 0; u < kRows; ++u) {
-          if (r0 + u * at.down < at.piece.rows) {
-            const float q = before_activation<ACT>(d[u].v[c], v[u].v[c], f.mean[c], f.rstd[c], f.w[c], f.b[c]);
-            s1 += q;
-            s2 = fmaf(q, (v[u].v[c] - f.mean[c]) * f.rstd[c], s2);
-          }
-        }
-        total[c].x += s1;
-        total[c].y += s2;
-      }
+      for (int u = 0; u < kRows; ++u) some.add(v[u], d[u], f);
+      all.add(some);
     }
+    for (; rows > 0; --rows, x += pace, dy += pace) all.add(load_channels<X, VEC>(x), load_channels<Y, VEC>(dy), f);
+    all.put(total);
   }
 #pragma unroll
   for (int c = 0; c < VEC; ++c) parts[c * kNormThreads + threadIdx.x] = total[c];
@@ -74,43 +119,16 @@ __global__ void __launch_bounds__(kNormThreads) norm_sums_kernel(NormArgs a, Nor
 
 constexpr int kJoinThreads = 512;
 
-// (A, B) of a group from its pieces' sums, in 64 bits: `lanes` threads (a power of two) along its channels, the others along
-// the pieces.
-__device__ __forceinline__ void join_means(const NormArgs& a, const NormShape& sh, const int32_t* first, const float2* partial,
-                                           float2* means, int32_t lanes, int64_t pair, int32_t thread, int32_t threads, bool warp) {
-  const int64_t graph = pair / a.groups;
-  const int32_t group = (int32_t)(pair % a.groups);
-  const Rows r = rows_of(a, graph);
-  const int32_t lo = first ? first[graph] : 0, hi = first ? first[graph + 1] : sh.pieces;
-  const int32_t down = threads / lanes;
-  double s1 = 0.0, s2 = 0.0;
-  for (int32_t k = thread % lanes; k < a.width; k += lanes) {
-    const int32_t channel = group * a.width + k;
-    const double w = a.weight ? a.weight[channel] : 1.f;
-    double t1 = 0.0, t2 = 0.0;
-#pragma unroll 4
-    for (int32_t p = lo + thread / lanes; p < hi; p += down) {
-      const float2 v = partial[(int64_t)p * a.F + channel];
-      t1 += v.x;
-      t2 += v.y;
-    }
-    s1 += w * t1;
-    s2 += w * t2;
-  }
-  s1 = warp ? warp_sum(s1) : block_sum(s1);
-  s2 = warp ? warp_sum(s2) : block_sum(s2);
-  const double n = r.hi > r.lo ? (double)(r.hi - r.lo) * a.width : 1.0;
-  if (thread == 0) means[pair] = make_float2((float)(s1 / n), (float)(s2 / n));
-}
-
-// The gradients of weight and bias of 8 channels: 64 threads along the `rows` rows of sums.  In 64 bits.
-__device__ __forceinline__ void join_weights(int32_t F, const float2* partial, int64_t rows, float* dweight, float* dbias, int32_t tile) {
+// totals[graph][channel] = the sums of a graph's pieces, in 64 bits: blocks of 8 channels x 64 threads along the pieces where
+// there is one graph (their totals are the gradients of bias and weight too).
+__device__ __forceinline__ void join_channels(int32_t F, const float2* partial, int64_t lo, int64_t hi, float2* total, float* dweight,
+                                              float* dbias, int32_t tile) {
   __shared__ double2 sums[kJoinThreads];
   const int32_t c = tile * 8 + threadIdx.x % 8;
   double s1 = 0.0, s2 = 0.0;
   if (c < F) {
 #pragma unroll 8
-    for (int64_t p = threadIdx.x / 8; p < rows; p += kJoinThreads / 8) {
+    for (int64_t p = lo + threadIdx.x / 8; p < hi; p += kJoinThreads / 8) {
       const float2 v = partial[p * F + c];
       s1 += v.x;
       s2 += v.y;
@@ -125,31 +143,39 @@ __device__ __forceinline__ void join_weights(int32_t F, const float2* partial, i
     }
   }
   if (threadIdx.x >= 8 || c >= F) return;
-  if (dbias) dbias[c] = (float)sums[threadIdx.x].x;
-  if (dweight) dweight[c] = (float)sums[threadIdx.x].y;
+  const float2 r = make_float2((float)sums[threadIdx.x].x, (float)sums[threadIdx.x].y);
+  if (total) total[c] = r;
+  if (dbias) dbias[c] = r.x;
+  if (dweight) dweight[c] = r.y;
 }
-
-// One graph: a block for a group, then the blocks of the weights.
 __global__ void __launch_bounds__(kJoinThreads)
-    norm_join_sums_kernel(NormArgs a, NormShape sh, const float2* partial, float2* means, float* dweight, float* dbias, int32_t lanes) {
+    norm_join_sums_kernel(int32_t F, const float2* partial, int64_t rows, float2* total, float* dweight, float* dbias) {
   cudaGridDependencySynchronize();
-  const int32_t pairs = means ? a.groups : 0;
-  if (blockIdx.x < pairs)
-    join_means(a, sh, nullptr, partial, means, lanes, blockIdx.x, threadIdx.x, kJoinThreads, false);
-  else
-    join_weights(a.F, partial, sh.pieces, dweight, dbias, blockIdx.x - pairs);
+  join_channels(F, partial, 0, rows, total, dweight, dbias, blockIdx.x);
 }
-// Many graphs: a warp for a group.
+// Many graphs: a warp for a graph and 8 channels, 4 threads along the pieces.
 __global__ void __launch_bounds__(kNormThreads)
-    norm_join_means_kernel(NormArgs a, NormShape sh, const int32_t* first, const float2* partial, float2* means, int32_t lanes) {
+    norm_join_graphs_kernel(int32_t F, int64_t graphs, const int32_t* first, const float2* partial, float2* totals) {
   cudaGridDependencySynchronize();
-  const int64_t pair = (int64_t)blockIdx.x * (kNormThreads / 32) + threadIdx.x / 32;
-  if (pair < a.graphs * a.groups) join_means(a, sh, first, partial, means, lanes, pair, threadIdx.x % 32, 32, true);
-}
-__global__ void __launch_bounds__(kJoinThreads)
-    norm_weight_sums_kernel(int32_t F, const float2* partial, int64_t rows, float* dweight, float* dbias) {
-  cudaGridDependencySynchronize();
-  join_weights(F, partial, rows, dweight, dbias, blockIdx.x);
+  const int32_t tiles = (F + 7) / 8, lane = threadIdx.x & 31;
+  const int64_t item = (int64_t)blockIdx.x * (kNormThreads / 32) + threadIdx.x / 32, graph = item / tiles;
+  if (graph >= graphs) return;
+  const int32_t c = (int32_t)(item - graph * tiles) * 8 + lane % 8, hi = first[graph + 1];
+  double s1 = 0.0, s2 = 0.0;
+  if (c < F) {
+#pragma unroll 4
+    for (int32_t p = first[graph] + lane / 8; p < hi; p += 4) {
+      const float2 v = partial[(int64_t)p * F + c];
+      s1 += v.x;
+      s2 += v.y;
+    }
+  }
+#pragma unroll
+  for (int o = 16; o >= 8; o /= 2) {
+    s1 += __shfl_xor_sync(0xffffffffu, s1, o);
+    s2 += __shfl_xor_sync(0xffffffffu, s2, o);
+  }
+  if (lane < 8 && c < F) totals[graph * F + c] = make_float2((float)s1, (float)s2);
 }
 
 // Short graphs: sums, A and B and the results in one launch.  graph_sums[graph][channel] = (sum of d, sum of d hat), or, for
@@ -166,17 +192,12 @@ __global__ void __launch_bounds__(kGraphThreads, VEC == 8 ? 4 : 6)
   const Y* dy = static_cast<const Y*>(a.dY) + at.base;
   X* dx = static_cast<X*>(a.out) + at.base;
   const bool mine = at.channel < a.F;
-  int32_t group[VEC];
-  Fixed<VEC> f = {};
+  Fixed<VEC> f;
   if (mine) {
-#pragma unroll
-    for (int k = 0; k < VEC; ++k) {
-      group[k] = group_of(plan, at.channel - at.tile_first + k);
-      const float2 st = a.stats[(int64_t)at.graph * a.groups + first_group + group[k]];
-      f.mean[k] = st.x, f.rstd[k] = st.y;
-      f.w[k] = a.weight ? a.weight[at.channel + k] : 1.f;
-      f.b[k] = a.bias ? a.bias[at.channel + k] : 0.f;
-    }
+    fix_weights<VEC>(f, a, at.channel);
+    fix_stats<VEC>(f, [&](int c) {
+      return a.stats[(int64_t)at.graph * a.groups + first_group + group_of(plan, at.channel - at.tile_first + c)];
+    });
   }
   extern __shared__ uint4 slots[];
   RawChannels<X, VEC>* const v = reinterpret_cast<RawChannels<X, VEC>*>(slots) + threadIdx.x;
@@ -194,21 +215,17 @@ __global__ void __launch_bounds__(kGraphThreads, VEC == 8 ? 4 : 6)
       fetch<Y, VEC>(d + (place * kStep + u) * kGraphThreads, dy + from);
     }
   };
-  float2 total[VEC] = {};
+  Sums<ACT, VEC> all = {};
   ring_forward<kRing>(steps, fetch_rows, [&](int32_t q, int place) {
 #pragma unroll
     for (int u = 0; u < kStep; ++u) {
       if (q * kStep + u >= count) break;
       const int at_slot = (place * kStep + u) * kGraphThreads;
-      const Channels<VEC> vx = numbers_of(v[at_slot]), vd = numbers_of(d[at_slot]);
-#pragma unroll
-      for (int k = 0; k < VEC; ++k) {
-        const float q = before_activation<ACT>(vd.v[k], vx.v[k], f.mean[k], f.rstd[k], f.w[k], f.b[k]);
-        total[k].x += q;
-        total[k].y = fmaf(q, (vx.v[k] - f.mean[k]) * f.rstd[k], total[k].y);
-      }
+      all.add(numbers_of(v[at_slot]), numbers_of(d[at_slot]), f);
     }
   });
+  float2 total[VEC];
+  all.put(total);
   // parts[y][channel of the tile]
   const int32_t stride = sh.across * VEC;
   if (at.y < sh.down) {
@@ -285,71 +302,77 @@ __global__ void __launch_bounds__(kGraphThreads, VEC == 8 ? 4 : 6)
   if (cluster > 1) cluster_arrive();  // the others' shared memory has been read
   __syncthreads();
   if (mine && a.out) {
-    float A[VEC], B[VEC];
-#pragma unroll
-    for (int k = 0; k < VEC; ++k) {
-      const float2 m = group_means[group[k]];
-      A[k] = m.x, B[k] = m.y;
-    }
+    Two A[kPairs<VEC>], B[kPairs<VEC>];
+    means_of<VEC>(A, B, [&](int c) { return group_means[group_of(plan, at.channel - at.tile_first + c)]; });
     ring_back<kRing>(steps, fetch_rows, [&](int32_t q, int place) {
       X* to = dx + q * kStep * pace;
 #pragma unroll
       for (int u = 0; u < kStep; ++u, to += pace) {
         if (q * kStep + u >= count) break;
         const int at_slot = (place * kStep + u) * kGraphThreads;
-        const Channels<VEC> vx = numbers_of(v[at_slot]), vd = numbers_of(d[at_slot]);
-        Channels<VEC> r;
-#pragma unroll
-        for (int k = 0; k < VEC; ++k) {
-          const float q = before_activation<ACT>(vd.v[k], vx.v[k], f.mean[k], f.rstd[k], f.w[k], f.b[k]) * f.w[k];
-          const float hat = (vx.v[k] - f.mean[k]) * f.rstd[k];
-          r.v[k] = (q - A[k] - hat * B[k]) * f.rstd[k];
-        }
-        store_channels<X, VEC>(to, r);
+        store_channels<X, VEC>(to, gradient_of<ACT, VEC>(numbers_of(v[at_slot]), numbers_of(d[at_slot]), f, A, B));
       }
     });
   }
   if (cluster > 1) cluster_wait();
 }
 
+// As forward, from the last rows back.  A and B of the tile's groups come from the channels' totals, summed anew by every
+// block: a few hundred numbers from the L2, where a launch between would cost more.
 template <typename X, typename Y, int ACT, int VEC>
-__global__ void __launch_bounds__(kNormThreads) norm_apply_bwd_kernel(NormArgs a, NormShape sh, const Piece* pieces, const float2* means) {
+__global__ void __launch_bounds__(kNormThreads, VEC == 8 ? 2 : 3)
+    norm_apply_bwd_kernel(NormArgs a, NormShape sh, const Piece* pieces, const float2* totals) {
+  __shared__ float2 means[kNormThreads * VEC];  // of the groups that the tile touches: no more than its channels
   cudaGridDependencySynchronize();
-  const Place at = place_of(a, sh, pieces, gridDim.x - 1 - blockIdx.x);
-  if (at.channel >= a.F) return;
-  const Fixed<VEC> f = fixed_of<VEC>(a, at.piece.graph, at.channel);
-  float A[VEC], B[VEC];
-#pragma unroll
-  for (int c = 0; c < VEC; ++c) {
-    const float2 m = means[(int64_t)at.piece.graph * a.groups + (at.channel + c) / a.width];
-    A[c] = m.x, B[c] = m.y;
+  const Place at = place_of(a, sh, pieces, blockIdx.x);
+  const int32_t tile_first = blockIdx.y * sh.across * VEC, tile_end = min(tile_first + sh.across * VEC, a.F);
+  const int32_t first_group = tile_first / a.width, groups = (tile_end - 1) / a.width - first_group + 1;
+  const Rows graph_rows = rows_of(a, at.piece.graph);
+  const float n = (float)(graph_rows.hi - graph_rows.lo) * a.width;
+  const float2* mine = totals + (int64_t)at.piece.graph * a.F;
+  int32_t lanes = 1;
+  while (lanes < a.width && lanes < 32) lanes *= 2;
+  for (int32_t g0 = 0; g0 < groups; g0 += kNormThreads / lanes) {
+    const int32_t g = g0 + threadIdx.x / lanes;
+    float s1 = 0.f, s2 = 0.f;
+    if (g < groups) {
+      for (int32_t k = threadIdx.x % lanes; k < a.width; k += lanes) {
+        const int32_t channel = (first_group + g) * a.width + k;
+        const float2 t = mine[channel];
+        const float w = a.weight ? a.weight[channel] : 1.f;
+        s1 = fmaf(w, t.x, s1);
+        s2 = fmaf(w, t.y, s2);
+      }
+    }
+    for (int o = lanes / 2; o > 0; o /= 2) {
+      s1 += __shfl_xor_sync(0xffffffffu, s1, o);
+      s2 += __shfl_xor_sync(0xffffffffu, s2, o);
+    }
+    if (g < groups && threadIdx.x % lanes == 0) means[g] = make_float2(s1 / n, s2 / n);
   }
-  const int64_t base = (int64_t)at.piece.row * a.F + at.channel;
+  __syncthreads();
+  if (at.channel >= a.F || at.y >= at.piece.rows) return;
+  const Fixed<VEC> f = fixed_of<VEC>(a, at.piece.graph, at.channel);
+  Two A[kPairs<VEC>], B[kPairs<VEC>];
+  means_of<VEC>(A, B, [&](int c) { return means[(at.channel + c) / a.width - first_group]; });
+  int32_t rows = (at.piece.rows - at.y + at.down - 1) / at.down;
+  const int64_t pace = (int64_t)at.down * a.F;
+  const int64_t base = ((int64_t)at.piece.row + at.y) * a.F + at.channel + (rows - 1) * pace;
   const X* x = static_cast<const X*>(a.X) + base;
   const Y* dy = static_cast<const Y*>(a.dY) + base;
   X* dx = static_cast<X*>(a.out) + base;
-  for (int32_t r0 = at.y; r0 < at.piece.rows; r0 += at.down * kRows) {
+  for (; rows >= kRows; rows -= kRows, x -= kRows * pace, dy -= kRows * pace, dx -= kRows * pace) {
     Channels<VEC> v[kRows], d[kRows];
 #pragma unroll
     for (int u = 0; u < kRows; ++u) {
-      const int32_t r = r0 + u * at.down;
-      if (r < at.piece.rows) {
-        v[u] = load_channels<X, VEC>(x + (int64_t)r * a.F);
-        d[u] = load_channels<Y, VEC>(dy + (int64_t)r * a.F);
-      }
+      v[u] = load_channels<X, VEC>(x - u * pace);
+      d[u] = load_channels<Y, VEC>(dy - u * pace);
     }
 #pragma unroll
-    for (int u = 0; u < kRows; ++u) {
-      if (r0 + u * at.down >= at.piece.rows) break;
-#pragma unroll
-      for (int c = 0; c < VEC; ++c) {
-        const float q = before_activation<ACT>(d[u].v[c], v[u].v[c], f.mean[c], f.rstd[c], f.w[c], f.b[c]) * f.w[c];
-        const float hat = (v[u].v[c] - f.mean[c]) * f.rstd[c];
-        v[u].v[c] = (q - A[c] - hat * B[c]) * f.rstd[c];
-      }
-      store_channels<X, VEC>(dx + (int64_t)(r0 + u * at.down) * a.F, v[u]);
-    }
+    for (int u = 0; u < kRows; ++u) store_channels<X, VEC>(dx - u * pace, gradient_of<ACT, VEC>(v[u], d[u], f, A, B));
   }
+  for (; rows > 0; --rows, x -= pace, dy -= pace, dx -= pace)
+    store_channels<X, VEC>(dx, gradient_of<ACT, VEC>(load_channels<X, VEC>(x), load_channels<Y, VEC>(dy), f, A, B));
 }
 
 template <typename X, typename Y, int ACT>
@@ -427,11 +450,11 @@ dg_status_t backward(const Graph* g, const NormArgs& a, dg_type_t x, dg_type_t y
   const bool weights = dweight || dbias;
   if (!weights && !a.out) return DG_OK;
   const int vec = norm_vector(a, x, y);
-  const unsigned weight_blocks = (unsigned)((a.F + 7) / 8);
+  const unsigned channel_blocks = (unsigned)((a.F + 7) / 8);
   void* memory = nullptr;
   const GraphPlan plan = graph_plan(g, a, vec, sizeof(X), kSlots, false);
-  const size_t graph_bytes = weights && a.graphs > 1 ? (size_t)a.graphs * a.F * sizeof(float2) : 0;
-  if (plan.blocks > 0 && (!graph_bytes || scratch_alloc(g, graph_bytes, s, &memory) == cudaSuccess)) {
+  const size_t graph_bytes = a.graphs > 1 ? (size_t)a.graphs * a.F * sizeof(float2) : 0;
+  if (plan.blocks > 0 && (!weights || !graph_bytes || scratch_alloc(g, graph_bytes, s, &memory) == cudaSuccess)) {
     float2* sums = static_cast<float2*>(memory);
     cudaError_t e = by_vector<kWide>(vec, [&](auto v) {
       constexpr int VEC = decltype(v)::value;
@@ -439,17 +462,16 @@ dg_status_t backward(const Graph* g, const NormArgs& a, dg_type_t x, dg_type_t y
       return launch_graphs(plan, norm_graph_bwd_kernel<X, Y, ACT, VEC>, kBytes, s, a, sums, dweight, dbias);
     });
     if (e == cudaSuccess && sums)
-      e = launch_kernel(norm_weight_sums_kernel, dim3(weight_blocks), kJoinThreads, s, true, a.F, (const float2*)sums, a.graphs,
-                        dweight, dbias);
+      e = launch_kernel(norm_join_sums_kernel, dim3(channel_blocks), kJoinThreads, s, true, a.F, (const float2*)sums, a.graphs,
+                        (float2*)nullptr, dweight, dbias);
     pool_free(memory, s);
     DG_CUDA(e);
     count_launches(1 + (sums != nullptr));
     return DG_OK;
   }
   const NormShape sh = norm_shape(g, a, vec);
-  const size_t partial_bytes = (size_t)sh.pieces * a.F * sizeof(float2);
-  const int64_t pairs = a.out ? a.graphs * a.groups : 0;
-  if (plan.blocks > 0 || scratch_alloc(g, partial_bytes + (size_t)pairs * sizeof(float2), s, &memory) != cudaSuccess) {
+  const size_t partial_bytes = (size_t)sh.pieces * a.F * sizeof(float2), total_bytes = (size_t)a.graphs * a.F * sizeof(float2);
+  if (plan.blocks > 0 || scratch_alloc(g, partial_bytes + total_bytes, s, &memory) != cudaSuccess) {
     int across = 1;
     while (across < a.width && across < kNormThreads) across *= 2;
     if (weights)
@@ -460,34 +482,31 @@ dg_status_t backward(const Graph* g, const NormArgs& a, dg_type_t x, dg_type_t y
     return DG_OK;
   }
   float2* partial = static_cast<float2*>(memory);
-  float2* means = reinterpret_cast<float2*>(static_cast<char*>(memory) + partial_bytes);
+  float2* totals = reinterpret_cast<float2*>(static_cast<char*>(memory) + partial_bytes);
   const dim3 grid((unsigned)sh.pieces, (unsigned)sh.tiles);
   const Piece* pieces = g->batch_pieces;
+  const int64_t items = a.graphs * channel_blocks;  // of the join of many graphs: a warp each
   if (sh.pieces > 0)
     by_vector<kWide>(vec, [&](auto v) {
       norm_sums_kernel<X, Y, ACT, decltype(v)::value><<<grid, kNormThreads, 0, s>>>(a, sh, pieces, partial);
     });
   cudaError_t e = cudaGetLastError();
-  int32_t lanes = 1;
-  while (lanes < a.width && lanes < 32) lanes *= 2;
-  const bool together = !pieces;  // one graph: the weights' blocks ride along
-  if (e == cudaSuccess && together)
-    e = launch_kernel(norm_join_sums_kernel, dim3((unsigned)pairs + (weights ? weight_blocks : 0)), kJoinThreads, s, true, a, sh,
-                      (const float2*)partial, a.out ? means : (float2*)nullptr, dweight, dbias, lanes);
-  if (e == cudaSuccess && !together && a.out)
-    e = launch_kernel(norm_join_means_kernel, dim3((unsigned)((pairs + 7) / 8)), kNormThreads, s, true, a, sh, g->batch_first,
-                      (const float2*)partial, means, lanes);
+  if (e == cudaSuccess && pieces)
+    e = launch_kernel(norm_join_graphs_kernel, dim3((unsigned)((items + 7) / 8)), kNormThreads, s, true, a.F, a.graphs,
+                      g->batch_first, (const float2*)partial, totals);
+  // the gradients of weight and bias, and the totals where one graph has all pieces
+  if (e == cudaSuccess && (weights || !pieces))
+    e = launch_kernel(norm_join_sums_kernel, dim3(channel_blocks), kJoinThreads, s, true, a.F,
+                      (const float2*)(pieces ? totals : partial), pieces ? a.graphs : (int64_t)sh.pieces, pieces ? nullptr : totals,
+                      dweight, dbias);
   if (e == cudaSuccess && a.out && sh.pieces > 0)
     e = by_vector<kWide>(vec, [&](auto v) {
       return launch_kernel(norm_apply_bwd_kernel<X, Y, ACT, decltype(v)::value>, grid, kNormThreads, s, true, a, sh, pieces,
-                           (const float2*)means);
+                           (const float2*)totals);
     });
-  if (e == cudaSuccess && !together && weights)
-    e = launch_kernel(norm_weight_sums_kernel, dim3(weight_blocks), kJoinThreads, s, true, a.F, (const float2*)partial,
-                      (int64_t)sh.pieces, dweight, dbias);
   pool_free(memory, s);
   DG_CUDA(e);
-  count_launches((sh.pieces > 0) + (together ? 1 : weights + (a.out != nullptr)) + (a.out && sh.pieces > 0));
+  count_launches((sh.pieces > 0) + (pieces != nullptr) + (weights || !pieces) + (a.out && sh.pieces > 0));
   return DG_OK;
 }
 
