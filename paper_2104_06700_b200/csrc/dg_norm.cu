@@ -126,7 +126,7 @@ __global__ void __launch_bounds__(kNormThreads, VEC == 8 ? 3 : 4)
 #pragma unroll
       for (int u = 0; u < kStep; ++u) {
         if (u >= few) break;
-        const Channels<VEC> v = load_channels<X, VEC>(x + u * pace);
+        const Channels<VEC> v = load_channels<X, VEC, false>(x + u * pace);
 #pragma unroll
         for (int c = 0; c < VEC; ++c) mean.v[c] += v.v[c];
       }
@@ -142,14 +142,21 @@ __global__ void __launch_bounds__(kNormThreads, VEC == 8 ? 3 : 4)
       for (int k = 0; k < kP; ++k) from[k] = pair_of(mean, k) * both(inverse);
     }
     int32_t r = 0;
-    for (; r + kStatRows <= rows; r += kStatRows, x += kStatRows * pace) {
+    for (; r + kStatRows <= rows - sh.kept; r += kStatRows, x += kStatRows * pace) {
       Channels<VEC> v[kStatRows];
 #pragma unroll
-      for (int u = 0; u < kStatRows; ++u) v[u] = load_channels<X, VEC>(x + u * pace);
+      for (int u = 0; u < kStatRows; ++u) v[u] = load_channels<X, VEC, true>(x + u * pace);
 #pragma unroll
       for (int u = 0; u < kStatRows; ++u) add(v[u]);
     }
-    for (; r < rows; ++r, x += pace) add(load_channels<X, VEC>(x));
+    for (; r + kStatRows <= rows; r += kStatRows, x += kStatRows * pace) {
+      Channels<VEC> v[kStatRows];
+#pragma unroll
+      for (int u = 0; u < kStatRows; ++u) v[u] = load_channels<X, VEC, false>(x + u * pace);
+#pragma unroll
+      for (int u = 0; u < kStatRows; ++u) add(v[u]);
+    }
+    for (; r < rows; ++r, x += pace) add(load_channels<X, VEC, false>(x));
     Channels<VEC> s, q, f;
 #pragma unroll
     for (int k = 0; k < kP; ++k) set_pair(s, k, sum[k]), set_pair(q, k, squares[k]), set_pair(f, k, from[k]);
@@ -352,7 +359,7 @@ __global__ void norm_join_kernel(NormArgs a, NormShape sh, const Piece* pieces, 
 // their ends.
 template <typename X, typename Y, int ACT, int VEC>
 __global__ void __launch_bounds__(kNormThreads, VEC == 8 ? 3 : 4) norm_apply_kernel(NormArgs a, NormShape sh, const Piece* pieces) {
-  constexpr int kRows = 4;
+  constexpr int kRows = sizeof(X) * VEC == 16 ? 4 : 8;  // in flight
   cudaGridDependencySynchronize();
   const Place at = place_of(a, sh, pieces, blockIdx.x);
   if (at.channel >= a.F || at.y >= at.piece.rows) return;
@@ -365,7 +372,7 @@ __global__ void __launch_bounds__(kNormThreads, VEC == 8 ? 3 : 4) norm_apply_ker
   for (; rows >= kRows; rows -= kRows, x -= kRows * pace, y -= kRows * pace) {
     Channels<VEC> v[kRows];
 #pragma unroll
-    for (int u = 0; u < kRows; ++u) v[u] = load_channels<X, VEC>(x - u * pace);
+    for (int u = 0; u < kRows; ++u) v[u] = load_channels<X, VEC, true>(x - u * pace);
 #pragma unroll
     for (int u = 0; u < kRows; ++u) {
       normalise<ACT, VEC>(v[u], f);
@@ -373,7 +380,7 @@ __global__ void __launch_bounds__(kNormThreads, VEC == 8 ? 3 : 4) norm_apply_ker
     }
   }
   for (; rows > 0; --rows, x -= pace, y -= pace) {
-    Channels<VEC> v = load_channels<X, VEC>(x);
+    Channels<VEC> v = load_channels<X, VEC, true>(x);
     normalise<ACT, VEC>(v, f);
     store_channels<Y, VEC>(y, v);
   }
@@ -418,7 +425,7 @@ dg_status_t forward(const Graph* g, const NormArgs& a, dg_type_t x, dg_type_t y,
     count_launches(1);
     return DG_OK;
   }
-  const NormShape sh = norm_shape(g, a, vec);
+  const NormShape sh = norm_shape(g, a, vec, sizeof(X), vec == 8 ? 3 : 4);
   const int32_t units = shared ? a.F / vec : a.F;
   void* memory = nullptr;
   if (sh.pieces > 0 && scratch_alloc(g, (size_t)sh.pieces * units * sizeof(float2), s, &memory) != cudaSuccess) {
@@ -540,7 +547,7 @@ GraphPlan graph_plan(const Graph* g, const NormArgs& a, int vec, int x_bytes, in
   return plan;
 }
 
-NormShape norm_shape(const Graph* g, const NormArgs& a, int vec) {
+NormShape norm_shape(const Graph* g, const NormArgs& a, int vec, int cell_bytes, int blocks_per_sm) {
   NormShape sh{};
   sh.vec = vec;
   const int32_t vectors = a.F / vec;
@@ -556,17 +563,20 @@ NormShape norm_shape(const Graph* g, const NormArgs& a, int vec) {
     }
     if (tiles >= 4 + (vectors + kNormThreads - 1) / kNormThreads) break;
   }
-  if (g->batch_pieces || a.offsets) {
+  if (g->batch_pieces) {
     sh.pieces = g->batch_piece_count;
+    sh.kept = INT32_MAX / 2;  // the graphs' pieces come in several waves
     return sh;
   }
-  // one wave of the kernels that keep four blocks on an SM, two of those that keep two
-  const int64_t blocks = (int64_t)g->sm_count * 4 / sh.tiles;
+  // one wave: then every block reads its piece forward and back, and the L2 holds the end of each
+  const int64_t blocks = (int64_t)g->sm_count * blocks_per_sm / sh.tiles;
   int64_t rows = (a.rows + blocks - 1) / (blocks > 0 ? blocks : 1);
   const int64_t least = (int64_t)sh.down * 8;
   if (rows < least) rows = least;
   sh.rows = (int32_t)rows;
   sh.pieces = (int32_t)((a.rows + rows - 1) / rows);
+  const int64_t kept = (int64_t)(g->l2_bytes / 2) / ((int64_t)a.F * cell_bytes * (sh.pieces > 0 ? sh.pieces : 1)) / sh.down;
+  sh.kept = (int32_t)(kept < rows ? kept : rows);
   return sh;
 }
 

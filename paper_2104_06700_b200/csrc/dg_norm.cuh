@@ -104,6 +104,7 @@ struct NormShape {
   int32_t across, down, tiles;
   int32_t rows;      // of a piece where one graph has all rows
   int32_t pieces;
+  int32_t kept;      // of a thread's rows, the last ones: what the L2 still holds of the first pass in the second
 };
 
 constexpr int kNormThreads = 256;
@@ -113,25 +114,30 @@ template <int VEC>
 struct Channels {
   float v[VEC];
 };
-template <typename T, int VEC>
+// ONCE: the L2 need not keep them.
+template <typename T, int VEC, bool ONCE>
 __device__ __forceinline__ Channels<VEC> load_channels(const T* p) {
+  auto get = [](const auto* q) {
+    if constexpr (ONCE) return __ldcs(q);
+    else return *q;
+  };
   Channels<VEC> r;
   if constexpr (sizeof(T) == 4 && VEC == 4) {
-    const float4 q = *reinterpret_cast<const float4*>(p);
+    const float4 q = get(reinterpret_cast<const float4*>(p));
     r.v[0] = q.x, r.v[1] = q.y, r.v[2] = q.z, r.v[3] = q.w;
   } else if constexpr (sizeof(T) == 4 && VEC == 2) {
-    const float2 q = *reinterpret_cast<const float2*>(p);
+    const float2 q = get(reinterpret_cast<const float2*>(p));
     r.v[0] = q.x, r.v[1] = q.y;
   } else if constexpr (sizeof(T) == 2 && VEC >= 2) {
     uint32_t w[VEC / 2];
     if constexpr (VEC == 8) {
-      const uint4 q = *reinterpret_cast<const uint4*>(p);
+      const uint4 q = get(reinterpret_cast<const uint4*>(p));
       w[0] = q.x, w[1] = q.y, w[2] = q.z, w[3] = q.w;
     } else if constexpr (VEC == 4) {
-      const uint2 q = *reinterpret_cast<const uint2*>(p);
+      const uint2 q = get(reinterpret_cast<const uint2*>(p));
       w[0] = q.x, w[1] = q.y;
     } else {
-      w[0] = *reinterpret_cast<const uint32_t*>(p);
+      w[0] = get(reinterpret_cast<const uint32_t*>(p));
     }
 #pragma unroll
     for (int i = 0; i < VEC / 2; ++i) {
@@ -140,7 +146,10 @@ __device__ __forceinline__ Channels<VEC> load_channels(const T* p) {
     }
   } else {
     static_assert(VEC == 1, "one number");
-    r.v[0] = as_float(*p);
+    if constexpr (sizeof(T) == 4)
+      r.v[0] = get(p);
+    else
+      r.v[0] = __uint_as_float((uint32_t)get(reinterpret_cast<const unsigned short*>(p)) << 16);
   }
   return r;
 }
@@ -356,7 +365,7 @@ __device__ __forceinline__ Place place_of(const NormArgs& a, const NormShape& sh
 }
 
 // How a call's matrices are shared out among blocks.
-NormShape norm_shape(const Graph* g, const NormArgs& a, int vec);
+NormShape norm_shape(const Graph* g, const NormArgs& a, int vec, int cell_bytes, int blocks_per_sm);
 // The widest vectors that rows of F numbers and these pointers allow.
 int norm_vector(const NormArgs& a, dg_type_t x, dg_type_t y);
 

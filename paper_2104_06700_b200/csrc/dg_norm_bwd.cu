@@ -78,19 +78,23 @@ __global__ void __launch_bounds__(kNormThreads, VEC == 8 ? 2 : 3)
     const X* x = static_cast<const X*>(a.X) + base;
     const Y* dy = static_cast<const Y*>(a.dY) + base;
     Sums<ACT, VEC> all = {};
-    for (; rows >= kRows; rows -= kRows, x += kRows * pace, dy += kRows * pace) {
+    auto step = [&](auto once) {
+      constexpr bool kOnce = decltype(once)::value;
       Channels<VEC> v[kRows], d[kRows];
 #pragma unroll
       for (int u = 0; u < kRows; ++u) {
-        v[u] = load_channels<X, VEC>(x + u * pace);
-        d[u] = load_channels<Y, VEC>(dy + u * pace);
+        v[u] = load_channels<X, VEC, kOnce>(x + u * pace);
+        d[u] = load_channels<Y, VEC, kOnce>(dy + u * pace);
       }
       Sums<ACT, VEC> some = {};
 #pragma unroll
       for (int u = 0; u < kRows; ++u) some.add(v[u], d[u], f);
       all.add(some);
-    }
-    for (; rows > 0; --rows, x += pace, dy += pace) all.add(load_channels<X, VEC>(x), load_channels<Y, VEC>(dy), f);
+      rows -= kRows, x += kRows * pace, dy += kRows * pace;
+    };
+    while (rows >= kRows + sh.kept) step(std::true_type());
+    while (rows >= kRows) step(std::false_type());
+    for (; rows > 0; --rows, x += pace, dy += pace) all.add(load_channels<X, VEC, false>(x), load_channels<Y, VEC, false>(dy), f);
     all.put(total);
   }
 #pragma unroll
@@ -365,14 +369,14 @@ __global__ void __launch_bounds__(kNormThreads, VEC == 8 ? 2 : 3)
     Channels<VEC> v[kRows], d[kRows];
 #pragma unroll
     for (int u = 0; u < kRows; ++u) {
-      v[u] = load_channels<X, VEC>(x - u * pace);
-      d[u] = load_channels<Y, VEC>(dy - u * pace);
+      v[u] = load_channels<X, VEC, true>(x - u * pace);
+      d[u] = load_channels<Y, VEC, true>(dy - u * pace);
     }
 #pragma unroll
     for (int u = 0; u < kRows; ++u) store_channels<X, VEC>(dx - u * pace, gradient_of<ACT, VEC>(v[u], d[u], f, A, B));
   }
   for (; rows > 0; --rows, x -= pace, dy -= pace, dx -= pace)
-    store_channels<X, VEC>(dx, gradient_of<ACT, VEC>(load_channels<X, VEC>(x), load_channels<Y, VEC>(dy), f, A, B));
+    store_channels<X, VEC>(dx, gradient_of<ACT, VEC>(load_channels<X, VEC, true>(x), load_channels<Y, VEC, true>(dy), f, A, B));
 }
 
 template <typename X, typename Y, int ACT>
@@ -469,7 +473,7 @@ dg_status_t backward(const Graph* g, const NormArgs& a, dg_type_t x, dg_type_t y
     count_launches(1 + (sums != nullptr));
     return DG_OK;
   }
-  const NormShape sh = norm_shape(g, a, vec);
+  const NormShape sh = norm_shape(g, a, vec, sizeof(X) + sizeof(Y), vec == 8 ? 2 : 3);
   const size_t partial_bytes = (size_t)sh.pieces * a.F * sizeof(float2), total_bytes = (size_t)a.graphs * a.F * sizeof(float2);
   if (plan.blocks > 0 || scratch_alloc(g, partial_bytes + total_bytes, s, &memory) != cudaSuccess) {
     int across = 1;
