@@ -2,7 +2,7 @@
 Parameters), as the composite workload the epoch-time metric is quoted on.
 
 libdgagg runs the aggregation with the own row, the matrix products of large layers, the elementwise passes
-of a layer and the loss; the products of small layers and Adam are torch's.  Per layer  z_v = (sum_{u in N(v)} h_u + h_v) / (deg(v) + 1),
+of a layer, group norms between layers, the loss and the AdamW step; the products of small layers and Adam are torch's.  Per layer  z_v = (sum_{u in N(v)} h_u + h_v) / (deg(v) + 1),
 h'_v = act(z_v W + b)  (aggregate first, then the Linear: Table 8 of the paper lists the aggregation
 widths 100, 256, 256 for the 3-layer model, i.e. the layers' input widths), ReLU between layers, none
 after the last, softmax cross-entropy on a training mask, Adam.  The features need no gradient, so an
@@ -15,7 +15,7 @@ from typing import List, Sequence
 
 import torch
 
-from . import binding
+from . import binding, optim
 
 
 class _Aggregate(torch.autograd.Function):
@@ -163,6 +163,53 @@ class _GcnLayer(torch.autograd.Function):
         return dM, dW, db if needs[2] else None, None, None, None, None, None
 
 
+ACTIVATIONS = {"none": binding.DG_ACT_NONE, "relu": binding.DG_ACT_RELU, "silu": binding.DG_ACT_SILU}
+
+
+class _GroupNorm(torch.autograd.Function):
+    """dg_group_norm_fwd, and dg_group_norm_bwd in the backward pass."""
+
+    @staticmethod
+    def forward(ctx, X, weight, bias, graph, groups: int, eps: float, act: int, dtype):
+        X = X.contiguous()
+        weight, bias = (None if t is None else t.contiguous() for t in (weight, bias))
+        Y, stats = graph.dg_group_norm_fwd(X, groups, weight, bias, eps, act, y_dtype=dtype)
+        ctx.graph, ctx.groups, ctx.act, ctx.batch = graph, groups, act, graph.batch
+        ctx.save_for_backward(X, weight, bias, stats)
+        return Y
+
+    @staticmethod
+    @torch.autograd.function.once_differentiable
+    def backward(ctx, dY: torch.Tensor):
+        X, weight, bias, stats = ctx.saved_tensors
+        if ctx.graph.batch is not ctx.batch:
+            raise RuntimeError("dg_graph_set_batch was called between this norm's forward and backward pass")
+        needs = ctx.needs_input_grad
+        grads = ctx.graph.dg_group_norm_bwd(dY.contiguous(), X, stats, ctx.groups, weight, bias, ctx.act, want_dX=needs[0],
+                                            want_dweight=needs[1], want_dbias=needs[2])
+        return (*grads, None, None, None, None, None)
+
+
+class GroupNorm(torch.nn.Module):
+    """Group norm with an activation over the vertices of every graph of the handle's batch: act(norm(X) weight + bias).
+    ``groups`` = 1: layer norm of a graph, ``groups`` = channels: instance norm.  fp32 or bf16 in; out as in, or ``dtype``.
+    Vertices behind the batch's last graph come out as zeros.  Differentiable once."""
+
+    def __init__(self, graph: "binding.Graph", channels: int, groups: int, activation: str = "relu", eps: float = 1e-5,
+                 affine: bool = True):
+        super().__init__()
+        if groups < 1 or channels % groups:
+            raise ValueError(f"groups must divide {channels}, got {groups}")
+        if activation not in ACTIVATIONS:
+            raise ValueError(f"activation must be one of {sorted(ACTIVATIONS)}, got {activation!r}")
+        self.graph, self.groups, self.activation, self.eps = graph, groups, activation, eps
+        self.weight = torch.nn.Parameter(torch.ones(channels)) if affine else None
+        self.bias = torch.nn.Parameter(torch.zeros(channels)) if affine else None
+
+    def forward(self, X: torch.Tensor, dtype=None) -> torch.Tensor:
+        return _GroupNorm.apply(X, self.weight, self.bias, self.graph, self.groups, self.eps, ACTIVATIONS[self.activation], dtype)
+
+
 class _CrossEntropy(torch.autograd.Function):
     """torch's cross_entropy(logits[index], labels[index]) in two kernels forward and one backward."""
 
@@ -227,11 +274,20 @@ class GraphSAGE(torch.nn.Module):
     A layer runs as one autograd function on its Linear's parameters; where that Linear has hooks, no bias,
     another type (a parametrization, a module put in its place) or runs under autocast, the module itself is
     called between the aggregation and the activation.
+
+    ``norm_groups``: a GroupNorm of that many groups with ``activation`` ("relu", "silu" or "none") behind every layer but
+    the last, in the ReLU's place.  With ``bf16_aggregate`` it hands the next layer the bf16 rows that its aggregation gathers
+    (the own row is rounded with them), where that layer aggregates first.
     """
 
     def __init__(self, graph: "binding.Graph", dims: Sequence[int], project_first: bool = False,
-                 bf16_aggregate: bool = False, fused_aggregator: bool = False):
+                 bf16_aggregate: bool = False, fused_aggregator: bool = False, norm_groups: int = 0,
+                 activation: str = "relu"):
         super().__init__()
+        if not norm_groups and activation != "relu":
+            raise ValueError("activation goes with norm_groups; without norms it is the ReLU")
+        self.norms = torch.nn.ModuleList(
+            [GroupNorm(graph, d, norm_groups, activation) for d in dims[1:-1]] if norm_groups else [])
         self.graph = graph
         self.project_first = project_first
         self.bf16_aggregate = bf16_aggregate   # aggregate bf16-rounded activations (even widths)
@@ -249,30 +305,52 @@ class GraphSAGE(torch.nn.Module):
     def forward(self, H: torch.Tensor) -> torch.Tensor:
         for i, lin in enumerate(self.lin):
             project = self.project_first and lin.out_features < lin.in_features
-            relu = i + 1 < len(self.lin)
+            relu = i + 1 < len(self.lin) and not self.norms
             if _is_plain(lin):
                 width = lin.out_features if project else lin.in_features
                 H = _GcnLayer.apply(H, lin.weight, lin.bias, self.graph, self.inv_deg1, relu, project,
                                     self.bf16_aggregate and width % 2 == 0)
-                continue
-            if project:
+            elif project:
                 H = self._aggregated(torch.nn.functional.linear(H, lin.weight)) + lin.bias
             else:
                 H = lin(self._aggregated(H))
-            H = torch.relu(H) if relu else H
+            if self.norms and i + 1 < len(self.lin):
+                H = self.norms[i](H, self._input_type(i + 1))
+            elif relu and not _is_plain(lin):
+                H = torch.relu(H)
         return H
+
+    def _input_type(self, i: int):
+        """What layer i takes from a norm: bf16 where it rounds its input anyway."""
+        lin = self.lin[i]
+        project = self.project_first and lin.out_features < lin.in_features
+        return torch.bfloat16 if self.bf16_aggregate and not project and lin.in_features % 2 == 0 else torch.float32
 
     def _aggregated(self, M: torch.Tensor) -> torch.Tensor:
         return _gcn(self.graph, M, self.inv_deg1, self.bf16_aggregate and M.shape[1] % 2 == 0)
 
 
 def make_epoch(model: GraphSAGE, X: torch.Tensor, labels: torch.Tensor, train_idx: torch.Tensor,
-               lr: float = 0.01, weight_decay: float = 5e-4):
+               lr: float = 0.01, weight_decay: float = 5e-4, optimizer: str = "adam", state_bits: int = 32,
+               max_norm=None):
     """Returns a function that runs one training epoch (forward, loss on the training vertices,
-    backward, Adam step) and returns the loss tensor."""
-    # one kernel for all parameters where they are on a GPU: a small graph's epoch is host time
-    opt = torch.optim.Adam(model.parameters(), lr=lr, weight_decay=weight_decay,
-                           fused=all(p.is_cuda for p in model.parameters()))
+    backward, optimiser step) and returns the loss tensor.
+
+    ``optimizer``: "adam" (torch's, weight decay in the gradient) or "adamw" (optim.AdamW: decoupled weight decay, ``state_bits``
+    32 or 8, gradients clipped to ``max_norm``).  "adamw" also learns the features ``X`` where they require a gradient; bf16
+    ones (for a model with ``bf16_aggregate``) get fp32 master weights.  The function's ``optimizer`` is the optimiser."""
+    if optimizer == "adamw":
+        learned = [X] if X.requires_grad else []
+        opt = optim.AdamW([*model.parameters(), *learned], lr=lr, weight_decay=weight_decay, state_bits=state_bits,
+                          max_norm=max_norm, master_weights=True)
+    elif optimizer != "adam":
+        raise ValueError(f"optimizer must be 'adam' or 'adamw', got {optimizer!r}")
+    elif state_bits != 32 or max_norm is not None:
+        raise ValueError("state_bits and max_norm go with optimizer='adamw'")
+    else:
+        # one kernel for all parameters where they are on a GPU: a small graph's epoch is host time
+        opt = torch.optim.Adam(model.parameters(), lr=lr, weight_decay=weight_decay,
+                               fused=all(p.is_cuda for p in model.parameters()))
 
     n = model.graph.n
     # vertex indices and class indices, one row of logits each; masks, probabilities and the like are torch's
@@ -297,6 +375,7 @@ def make_epoch(model: GraphSAGE, X: torch.Tensor, labels: torch.Tensor, train_id
         opt.step()
         return loss.detach()
 
+    epoch.optimizer = opt
     return epoch
 
 
