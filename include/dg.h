@@ -308,7 +308,8 @@ dg_status_t dg_cross_entropy_bwd(dg_graph_t g, const float* logits, int32_t C, c
  *   grad        fp32 or bf16 (grad_type), read only
  *   exp_avg, exp_avg_sq  state_bits = 32: m and v, fp32.  state_bits = 8: m and sqrt(v), e4m3 bytes, times the scales; rounded
  *               up or down at random, a sqrt(v) > 0 never to 0.  A number that is not finite becomes NaN and leaves the rest
- *               of its block alone
+ *               of its block alone.  What is rounded comes of the formulas operation by operation, each rounded to fp32, so that
+ *               other fp32 arithmetic arrives at the same codes and scales
  *   scales      state_bits = 8: 2 fp32 for every 256 numbers begun (of m, of sqrt(v)), 8-byte aligned; else NULL, and the array
  *               itself may be NULL where all are
  *   step        steps taken so far; read, then increased by 1 by the call (one number for each tensor)

@@ -58,8 +58,7 @@ static_assert(sizeof(Workspace) <= DG_ADAMW_WORKSPACE_BYTES, "dg.h promises less
 
 struct Hyper {
   double lr, log2_beta1, log2_beta2;
-  float beta1, rest1, beta2, rest2, eps, decay;  // beta1, 1 - beta1, beta2, 1 - beta2, eps, 1 - lr wd
-  float root2, root_rest2;                       // sqrt(beta2), sqrt(1 - beta2)
+  float rest1, beta2, rest2, eps, decay;  // 1 - beta1, beta2, 1 - beta2, eps, 1 - lr wd
 };
 
 // A 32-bit hash: lowbias32 of Chris Wellons.
@@ -175,12 +174,6 @@ __device__ __forceinline__ uint32_t to_bf16_random(float p, uint32_t r) {
   return (bits + (r & 0xffffu)) >> 16;
 }
 
-// off by at most 2^-23 of itself; numbers below 2^-126 count as 0
-__device__ __forceinline__ float fast_sqrt(float v) {
-  float r;
-  asm("sqrt.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(v));
-  return r;
-}
 // 1 / v, off by at most 2^-23 of itself
 __device__ __forceinline__ float fast_inverse(float v) {
   float r;
@@ -277,19 +270,23 @@ __device__ __forceinline__ void update(const Tensors<N>& a, int i, int64_t base,
     }
   }
   if constexpr (EIGHT) {
-    // scales and betas in one factor of each code
-    const Two keep_m = both(h.beta1 * in.scale.x), keep_u = both(h.root2 * in.scale.y);
-    const Two take_m = both(h.rest1 * factor), take_u = both(h.root_rest2 * factor);
+    // Operation by operation as the formulas have them, each rounded to nearest and none fused: which way an 8-bit number
+    // is rounded hangs on the last bit, a few numbers in a million go the other way when an operation is left out, and what
+    // they were is the next step's scale.  Any fp32 arithmetic that follows the formulas gets these codes.
+    const Two scale_m = both(in.scale.x), scale_u = both(in.scale.y), rest1 = both(h.rest1), rest2 = both(h.rest2);
+    const Two beta2 = both(h.beta2), factors = both(factor);
     float most_m = 0.f, most_u = 0.f;
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
-      const Two gj = two(g[2 * j], g[2 * j + 1]), now = gj * take_u;
-      const Two old = from_e4m3(in.v[j / 2] >> (16 * (j % 2))) * keep_u;
-      const Two mean = fma2(from_e4m3(in.m[j / 2] >> (16 * (j % 2))), keep_m, gj * take_m);
-      const float2 vj = apart(fma2(old, old, now * now)), mj = apart(mean);
-      v[2 * j] = fast_sqrt(vj.x), v[2 * j + 1] = fast_sqrt(vj.y);
+      const Two gj = two(g[2 * j], g[2 * j + 1]) * factors;
+      const Two old = from_e4m3(in.m[j / 2] >> (16 * (j % 2))) * scale_m, root = from_e4m3(in.v[j / 2] >> (16 * (j % 2))) * scale_u;
+      // The sums are single additions: ptxas makes one operation of a product and a sum of pairs.
+      const float2 mo = apart(old), step = apart(rest1 * (gj - old)), kept = apart(beta2 * (root * root)), taken = apart(rest2 * gj * gj);
+      const float2 mj = make_float2(__fadd_rn(mo.x, step.x), __fadd_rn(mo.y, step.y));
+      const float2 vj = make_float2(__fadd_rn(kept.x, taken.x), __fadd_rn(kept.y, taken.y));
+      v[2 * j] = __fsqrt_rn(vj.x), v[2 * j + 1] = __fsqrt_rn(vj.y);
       const float2 under = apart(fma2(two(v[2 * j], v[2 * j + 1]), both(st.c2), both(h.eps)));
-      const Two ratio = mean * two(fast_inverse(under.x), fast_inverse(under.y));
+      const Two ratio = two(mj.x, mj.y) * two(fast_inverse(under.x), fast_inverse(under.y));
       const float2 pj = apart(fma2(ratio, both(-st.c1), two(p[2 * j], p[2 * j + 1]) * both(h.decay)));
       p[2 * j] = pj.x, p[2 * j + 1] = pj.y;
       m[2 * j] = mj.x, m[2 * j + 1] = mj.y;
@@ -303,7 +300,8 @@ __device__ __forceinline__ void update(const Tensors<N>& a, int i, int64_t base,
       most_m = warp_most_finite(m);
       most_u = warp_most_finite(v);
     }
-    const float2 scale = make_float2(fmaxf(__fdiv_rn(most_m, kLargest), kLeastScale), fmaxf(__fdiv_rn(most_u, kLargest), kLeastScale));
+    const float2 scale = make_float2(fmaxf(__fmul_rn(most_m, 1.f / kLargest), kLeastScale),
+                                     fmaxf(__fmul_rn(most_u, 1.f / kLargest), kLeastScale));
     if (lane == 0) a.scales[i][base / kNumbers] = scale;
     const Two inv_m = both(__frcp_rn(scale.x)), inv_u = both(__frcp_rn(scale.y)), front = both(0x1p-120f);
     float ym[8], yu[8];
@@ -669,8 +667,8 @@ extern "C" dg_status_t dg_adamw_step(const dg_adamw_list_t* list, double lr, dou
   if (list->tensors == 0) return DG_OK;
   // an eps below the least normal number is that: its inverse has to be finite
   const float least = eps > 0.0 && eps < (double)kLeastScale ? kLeastScale : (float)eps;
-  const Hyper h{lr, log2(beta1), log2(beta2), (float)beta1, (float)(1.0 - beta1), (float)beta2, (float)(1.0 - beta2), least,
-                (float)(1.0 - lr * weight_decay), (float)sqrt(beta2), (float)sqrt(1.0 - beta2)};
+  const Hyper h{lr, log2(beta1), log2(beta2), (float)(1.0 - beta1), (float)beta2, (float)(1.0 - beta2), least,
+                (float)(1.0 - lr * weight_decay)};
   int sms = 0;
   if (dg_status_t st = device_sms(&sms)) return st;
   const StepCall c{h, grad_factor, seed, static_cast<Workspace*>(workspace), sms, (cudaStream_t)stream};
