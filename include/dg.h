@@ -293,8 +293,8 @@ dg_status_t dg_cross_entropy_bwd(dg_graph_t g, const float* logits, int32_t C, c
                                  const float* result, const float* grad, float* dLogits, void* stream);
 
 /*
- * AdamW over many tensors in one launch (one per 400 of them), and the norm of all gradients.  With
- * t = the tensor's steps so far + 1:
+ * AdamW over many tensors at once (a launch for the tensors of one kind - types and state_bits - and for 400 of them), and the
+ * norm of all gradients.  With t = the tensor's steps so far + 1:
  *
  *   g = grad * factor;  m = m + (1 - beta1) * (g - m);  v = beta2 * v + (1 - beta2) * g * g;
  *   param = param * (1 - lr * weight_decay) - lr / (1 - beta1^t) * m / (sqrt(v) / sqrt(1 - beta2^t) + eps)

@@ -145,7 +145,7 @@ def _holds(t: Optional[torch.Tensor], count: int, name: str) -> None:
 
 def _is_matrix(t: torch.Tensor, rows: int, columns: int, name: str) -> None:
     """A product is refused where its sizes do not fit: wider rows would be read as more of narrower ones."""
-    if tuple(t.shape) != (rows, columns):
+    if t.shape != (rows, columns):
         raise ValueError(f"{name} must be {rows} x {columns}, got {' x '.join(map(str, t.shape))}")
 
 
@@ -153,6 +153,10 @@ def _has(t: Optional[torch.Tensor], count: int, name: str) -> None:
     if t is not None and t.numel() != count:
         raise ValueError(f"{name} must have {count} values, got {t.numel()}")
 
+
+# for whole lists, by map: a long list of tensors is asked in one loop
+_data_ptr, _numel, _contiguous = torch.Tensor.data_ptr, torch.Tensor.numel, torch.Tensor.is_contiguous
+_get_device, _dtype, _layout = torch.Tensor.get_device, torch.Tensor.dtype.__get__, torch.Tensor.layout.__get__
 
 _TYPE_CODES = {torch.float32: DG_F32, torch.bfloat16: DG_BF16}
 
@@ -167,9 +171,10 @@ def _typed_ptr(t: torch.Tensor, name: str):
 
 def _on_current_device(**tensors) -> None:
     """A call's kernels run on the current device: every tensor has to be there."""
-    for name, t in tensors.items():
-        if t is not None and t.is_cuda and t.get_device() != _device():
-            raise ValueError(f"{name} is on {t.device}, the current device is cuda:{_device()}")
+    given = [t for t in tensors.values() if t is not None and t.is_cuda]
+    if given and not {_device()}.issuperset(map(_get_device, given)):
+        raise ValueError(f"the current device is cuda:{_device()}, but "
+                         + ", ".join(f"{k} is on {t.device}" for k, t in tensors.items() if t is not None))
 
 
 # The handle of the current stream of the current device.  torch.cuda.current_stream() builds two
@@ -237,8 +242,6 @@ def dg_permute_rows(new_of_old: torch.Tensor, x: torch.Tensor, to_old: bool = Fa
 
 DG_ADAMW_WORKSPACE_BYTES = 8192
 _FLOATS = (torch.float32, torch.bfloat16)
-_data_ptr, _numel, _contiguous = torch.Tensor.data_ptr, torch.Tensor.numel, torch.Tensor.is_contiguous
-_get_device, _dtype = torch.Tensor.get_device, torch.Tensor.dtype.__get__
 
 
 def _check_tensors(tensors, dtypes, device: int, name: str) -> list:
@@ -603,19 +606,21 @@ class Graph:
             raise ValueError("offsets must be at least two whole numbers")
         host = given.to("cpu", torch.int64).contiguous()
         _check(lib().dg_graph_set_batch(self._h, host.numel() - 1, host.data_ptr()))
-        self.batch = host.clone()
+        self.batch, self._batch_sizes = host.clone(), (host.numel() - 1, int(host[-1]))
 
-    def _norm_shapes(self, F, groups, weight, bias, **matrices):
+    def _norm_shapes(self, F, groups, weight, bias, stats, **matrices):
         """(graphs, rows that belong to a graph)"""
         for name, t in matrices.items():
-            if t is not None:
+            if t is not None and t.shape != (self.n, F):
                 _is_matrix(t, self.n, F, name)
         if groups < 1 or F % groups:
             raise ValueError(f"groups must divide {F}, got {groups}")
+        graphs, rows = (1, self.n) if self.batch is None else self._batch_sizes
         _has(weight, F, "weight")
         _has(bias, F, "bias")
-        _on_current_device(weight=weight, bias=bias, **matrices)
-        return (1, self.n) if self.batch is None else (self.batch.numel() - 1, int(self.batch[-1]))
+        _has(stats, graphs * groups * 2, "stats")
+        _on_current_device(weight=weight, bias=bias, stats=stats, **matrices)
+        return graphs, rows
 
     def _result(self, X, dtype, rows, stream):
         """A matrix like X, zeros in the rows behind `rows`: written on the stream that the call goes to."""
@@ -636,15 +641,13 @@ class Graph:
         Without ``Y`` a matrix of ``y_dtype`` (X's) is made, with zeros in the rows that belong to no graph; in a given one
         they stay as they are."""
         F = X.shape[1]
-        graphs, rows = self._norm_shapes(F, groups, weight, bias, X=X, Y=Y)
+        graphs, rows = self._norm_shapes(F, groups, weight, bias, stats, X=X, Y=Y)
         if Y is None:
             Y = self._result(X, y_dtype or X.dtype, rows, stream)
         elif y_dtype is not None and y_dtype != Y.dtype:
             raise TypeError(f"Y is {Y.dtype}, not {y_dtype}")
         if stats is None:
             stats = torch.empty((graphs, groups, 2), dtype=torch.float32, device=X.device)
-        _has(stats, graphs * groups * 2, "stats")
-        _on_current_device(stats=stats)
         (x, x_type), (y, y_type) = _typed_ptr(X, "X"), _typed_ptr(Y, "Y")
         _check(lib().dg_group_norm_fwd(self._h, x, x_type, F, int(groups), _dev_ptr(weight, torch.float32, "weight"),
                                        _dev_ptr(bias, torch.float32, "bias"), float(eps), int(act), y, y_type,
@@ -657,9 +660,7 @@ class Graph:
                           want_dweight: bool = True, want_dbias: bool = True, stream=None):
         """(dX, dweight, dbias), each None where it is not wanted.  Rows that belong to no graph: as in the forward call."""
         F = X.shape[1]
-        graphs, rows = self._norm_shapes(F, groups, weight, bias, X=X, dY=dY, dX=dX)
-        _has(stats, graphs * groups * 2, "stats")
-        _on_current_device(stats=stats)
+        graphs, rows = self._norm_shapes(F, groups, weight, bias, stats, X=X, dY=dY, dX=dX)
         if dX is None and want_dX:
             dX = self._result(X, X.dtype, rows, stream)
         elif dX is not None and dX.dtype != X.dtype:

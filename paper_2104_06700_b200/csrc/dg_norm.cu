@@ -419,6 +419,7 @@ dg_status_t forward(const Graph* g, const NormArgs& a, dg_type_t x, dg_type_t y,
     DG_CUDA((by_vector<sizeof(X) == 2 && sizeof(Y) == 2>(vec, [&](auto v) {
       constexpr int VEC = decltype(v)::value;
       constexpr size_t kBytes = (size_t)kSlots * kGraphThreads * VEC * sizeof(X);
+      static_assert(kBytes <= kMostPlaces, "ask for more shared memory");
       return shared ? launch_graphs(plan, norm_graph_kernel<X, Y, ACT, VEC, true>, kBytes, s, a)
                     : launch_graphs(plan, norm_graph_kernel<X, Y, ACT, VEC, false>, kBytes, s, a);
     })));

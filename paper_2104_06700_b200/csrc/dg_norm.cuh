@@ -64,17 +64,24 @@ __device__ __forceinline__ float activated(float z) {
   if constexpr (ACT == DG_ACT_SILU) return z * sigmoid(z);
   return z;
 }
-// Of a pair, with one reciprocal for both, that of the product: 2^63 is the most either factor may be, where 1 / (1 + exp(-z))
-// is of no account any more (hardware's functions bound these kernels: 2.4 M x 100 bf16, SiLU, forward: 285 us, 292 with two reciprocals).
+// Of a pair of numbers not below -43 (see above_floor), with one reciprocal for both, that of the product: hardware's
+// functions bound these kernels (2.4 M x 100 bf16, SiLU, forward: 285 us, 292 with two reciprocals).
 __device__ __forceinline__ Two sigmoid(Two z) {
   const float2 t = apart(z * both(-1.4426950408889634f));
   float2 e;
   float r;
-  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(e.x) : "f"(fminf(t.x, 62.f)));
-  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(e.y) : "f"(fminf(t.y, 62.f)));
+  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(e.x) : "f"(t.x));
+  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(e.y) : "f"(t.y));
   e = apart(two(e.x, e.y) + both(1.f));
   asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(e.x * e.y));
   return both(r) * two(e.y, e.x);
+}
+// z, or -43 below that: SiLU and its derivative are under 10^-17 there, and the product of two 1 + exp(-z) is finite.  NaN stays.
+__device__ __forceinline__ Two above_floor(Two z) {
+  float2 q = apart(z);
+  asm("max.NaN.f32 %0, %0, %1;" : "+f"(q.x) : "f"(-43.f));
+  asm("max.NaN.f32 %0, %0, %1;" : "+f"(q.y) : "f"(-43.f));
+  return two(q.x, q.y);
 }
 
 // dy act'(z).  The ReLU's border is where z changes its sign: near it (|hat w| is about |b| there and z is off by up to
@@ -179,6 +186,10 @@ __device__ __forceinline__ void store_channels(T* p, const Channels<VEC>& r) {
     *p = as<T>(r.v[0]);
   }
 }
+
+// What a kernel may have without asking the runtime for more (a microsecond of host time a call): 48 KiB, of which the
+// arrays beside the places take no more than 11.
+constexpr size_t kMostPlaces = (48 - 11) << 10;
 
 // VEC numbers as they are stored, from shared memory.
 template <typename T, int VEC>
@@ -312,7 +323,10 @@ __device__ __forceinline__ void normalise(Channels<VEC>& v, const Fixed<VEC>& f)
 #pragma unroll
   for (int k = 0; k < kPairs<VEC>; ++k) {
     Two z = fma2((pair_of(v, k) - f.mean[k]) * f.rstd[k], f.w[k], f.b[k]);
-    if constexpr (ACT == DG_ACT_SILU) z = z * sigmoid(z);
+    if constexpr (ACT == DG_ACT_SILU) {
+      z = above_floor(z);
+      z = z * sigmoid(z);
+    }
     if constexpr (ACT == DG_ACT_RELU) {
       const float2 q = apart(z);
       z = two(activated<ACT>(q.x), activated<ACT>(q.y));
@@ -328,8 +342,9 @@ __device__ __forceinline__ void backward_terms(Two x, Two dy, const Fixed<VEC>& 
   if constexpr (ACT == DG_ACT_NONE) {
     *d = dy;
   } else {
-    const Two z = fma2(*hat, f.w[k], f.b[k]);
+    Two z = fma2(*hat, f.w[k], f.b[k]);
     if constexpr (ACT == DG_ACT_SILU) {
+      z = above_floor(z);
       const Two s = sigmoid(z);
       *d = dy * (s * fma2(z, both(1.f) - s, both(1.f)));
     } else {
@@ -488,7 +503,6 @@ __device__ __forceinline__ float warp_total(float v) {
 template <typename... P, typename... A>
 cudaError_t launch_graphs(const GraphPlan& plan, void (*kernel)(NormArgs, GraphPlan, P...), size_t shared, cudaStream_t s,
                           const NormArgs& a, const A&... args) {
-  if (cudaError_t e = cudaFuncSetAttribute((const void*)kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)shared)) return e;
   cudaLaunchAttribute attribute{};
   attribute.id = cudaLaunchAttributeClusterDimension;
   attribute.val.clusterDim.x = 1u << plan.cluster_log;

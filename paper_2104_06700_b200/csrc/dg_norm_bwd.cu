@@ -463,6 +463,7 @@ dg_status_t backward(const Graph* g, const NormArgs& a, dg_type_t x, dg_type_t y
     cudaError_t e = by_vector<kWide>(vec, [&](auto v) {
       constexpr int VEC = decltype(v)::value;
       constexpr size_t kBytes = (size_t)kSlots * kGraphThreads * VEC * (sizeof(X) + sizeof(Y));
+      static_assert(kBytes <= kMostPlaces, "ask for more shared memory");
       return launch_graphs(plan, norm_graph_bwd_kernel<X, Y, ACT, VEC>, kBytes, s, a, sums, dweight, dbias);
     });
     if (e == cudaSuccess && sums)

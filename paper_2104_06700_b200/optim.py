@@ -50,6 +50,7 @@ class AdamW(torch.optim.Optimizer):
         super().add_param_group(group)
         params = self.param_groups[-1]["params"]
         if len(set(params)) != len(params):
+            self.param_groups.pop()
             raise ValueError("a parameter stands in its group twice: the one launch would update it twice at once")
 
     def __getstate__(self):     # workspaces are not state
@@ -104,9 +105,9 @@ class AdamW(torch.optim.Optimizer):
             for p, s in zip(params, states):
                 if not s:
                     s.update(self._new_state(p, group))
-        if any(g.layout is not torch.strided for g in grads):
+        if not {torch.strided}.issuperset(map(binding._layout, grads)):
             raise ValueError("sparse gradients are not supported")
-        if not all(map(torch.Tensor.is_contiguous, grads)):
+        if not all(map(binding._contiguous, grads)):
             grads = [g.contiguous() for g in grads]      # copies live until the launch, then the allocator's stream order serves
         columns = [[s["exp_avg"] for s in states], [s["exp_avg_sq"] for s in states], [s["step"] for s in states],
                    [s.get("scales") for s in states]]

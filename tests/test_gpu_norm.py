@@ -222,3 +222,95 @@ def test_no_rows():
     assert torch.allclose(stats[..., 1], torch.full_like(stats[..., 1], 1e-5 ** -0.5))
     dX, dw, db = g.dg_group_norm_bwd(X, X, stats, 2)
     assert dX.shape == (0, 8) and not bool(dw.any()) and not bool(db.any())
+
+
+def test_silu_far_below_zero():
+    """Where exp(-z) leaves fp32: results and gradients vanish, whatever the size of z."""
+    n, F = 3000, 8
+    X, dY, w, b = inputs(n, F, F32, F32, 8)
+    for big in (50.0, 1e3, 1e12, 1e30):
+        for offsets in ([0, n], [0, 20, n]):        # one graph in pieces' kernels and in a cluster's, and a batch
+            g = empty_graph(n)
+            if len(offsets) > 2:
+                g.dg_graph_set_batch(offsets)
+            bias = b - big
+            Y, stats = g.dg_group_norm_fwd(X, 2, w, bias, act=ACTS["silu"])
+            y, _, _, _ = norm_util.forward(X, offsets, 2, w, bias, 1e-5, "silu")
+            assert float((Y.double() - torch.nan_to_num(y)).abs().max()) <= 1e-12
+            dX, dw, db = g.dg_group_norm_bwd(dY, X, stats, 2, w, bias, ACTS["silu"])
+            assert all(float(t.abs().max()) <= 1e-10 for t in (dX, dw, db))
+            bias = b + big
+            Y, _ = g.dg_group_norm_fwd(X, 2, w, bias, act=ACTS["silu"])
+            assert bool(((Y.double() - (b.double() + big)).abs() <= 1e-6 * big + 100).all())
+
+
+def test_large_matrices_in_captured_graphs_and_two_streams():
+    """The kernels of long graphs take scratch between their launches: a replay, an eager call and another stream's call at
+    the same time do not share it."""
+    n, F, groups = 70000, 64, 4
+    X, dY, w, b = inputs(n, F, F32, BF16, 7)
+    g = empty_graph(n)
+    fwd = lambda X, **k: g.dg_group_norm_fwd(X, groups, w, b, act=ACTS["silu"], y_dtype=BF16, **k)  # noqa: E731
+    want = [fwd(X * s) for s in (1, 3)]
+    back = [g.dg_group_norm_bwd(dY, X * s, want[i][1], groups, w, b, ACTS["silu"]) for i, s in enumerate((1, 3))]
+    static = [X.clone(), X * 3]
+    graphs, outs = [], []
+    for i in range(2):
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph):
+            y = fwd(static[i])
+            outs.append((*y, *g.dg_group_norm_bwd(dY, static[i], y[1], groups, w, b, ACTS["silu"])))
+        graphs.append(graph)
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    for _ in range(5):
+        graphs[0].replay()
+        with torch.cuda.stream(side):
+            graphs[1].replay()
+        eager = fwd(static[0])
+        with torch.cuda.stream(side):
+            other = fwd(static[1])
+        torch.cuda.synchronize()
+        for i, e in enumerate((eager, other)):
+            for a, c in zip((*outs[i], *e), (*want[i], *back[i], *want[i])):
+                assert torch.equal(a, c)
+    del graphs
+
+
+def test_more_cells_than_32_bits_count():
+    n, F, groups = 9_000_000, 512, 8
+    X = torch.empty(n, F, dtype=BF16, device=DEV)
+    for lo in range(0, n, 1_000_000):
+        X[lo:lo + 1_000_000].normal_(0.1 * (lo % 3), 1 + lo / n)
+    dY = torch.empty_like(X).normal_(0, 0.1)
+    _, _, w, b = inputs(4, F, F32, F32, 9)
+    sums = torch.zeros(2, groups, dtype=torch.float64, device=DEV)
+    for lo in range(0, n, 250_000):
+        part = X[lo:lo + 250_000].double().view(-1, groups, F // groups)
+        sums += torch.stack([part.sum((0, 2)), part.square().sum((0, 2))])
+    mean = sums[0] / (n * (F // groups))
+    rstd = (sums[1] / (n * (F // groups)) - mean.square() + 1e-5).rsqrt()
+    for offsets in ([0, n], [0, 7, n - 2, n]):
+        g = empty_graph(n)
+        if len(offsets) > 2:
+            g.dg_graph_set_batch(offsets)
+        Y, stats = g.dg_group_norm_fwd(X, groups, w, b, act=ACTS["silu"])
+        if len(offsets) == 2:
+            # a thread adds some thousand rows: 2^-24 times their number at most, far less as roundings go both ways
+            assert float((stats[0, :, 0].double() - mean).abs().max()) <= 1e-5
+            assert float((stats[0, :, 1].double() / rstd - 1).abs().max()) <= 1e-5
+        dX, dw, db = g.dg_group_norm_bwd(dY, X, stats, groups, w, b, ACTS["silu"])
+        # the rows at both ends and about the places where 32-bit counts of cells end, from the statistics
+        st = stats[-1 if len(offsets) == 2 else 1].double()
+        for row in (10, 2 ** 31 // F - 3, 2 ** 32 // F - 3, n - 20):
+            x, hi = X[row:row + 6].double(), row + 6
+            hat = (x - st[:, 0].repeat_interleave(F // groups)) * st[:, 1].repeat_interleave(F // groups)
+            z = hat * w.double() + b.double()
+            y = z / (1 + torch.exp(-z))
+            assert bool(((Y[row:hi].double() - y).abs() <= 2.0 ** -8 * y.abs() + 1e-4).all())
+            s = torch.sigmoid(z)
+            q = dY[row:hi].double() * (s * (1 + z * (1 - s))) * w.double()
+            # A and B are means of nine million times 64 numbers of random sign: nearly nothing beside q
+            want = q * st[:, 1].repeat_interleave(F // groups)
+            assert bool(((dX[row:hi].double() - want).abs() <= 2.0 ** -8 * want.abs() + 2e-3 * (1 + hat.abs())).all())
+        del Y, dX
