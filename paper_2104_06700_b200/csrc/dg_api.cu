@@ -484,7 +484,7 @@ dg_status_t dg_graph_set_batch(dg_graph_t g, int64_t count, const int64_t* offse
   for (int64_t b = 0; b < count; ++b) pieces += (offsets[b + 1] - offsets[b] + rows - 1) / rows;
   const size_t offset_bytes = align256((size_t)(count + 1) * sizeof(int64_t));
   const size_t first_bytes = align256((size_t)(count + 1) * sizeof(int32_t));
-  const size_t order_bytes = align256((size_t)count * sizeof(int32_t));
+  const size_t order_bytes = align256((size_t)count * sizeof(Piece));
   const size_t bytes = offset_bytes + first_bytes + order_bytes + align256((size_t)pieces * sizeof(Piece));
   char* memory = nullptr;
   int32_t* lengths = nullptr;
@@ -505,10 +505,11 @@ dg_status_t dg_graph_set_batch(dg_graph_t g, int64_t count, const int64_t* offse
       const uint64_t p = *static_cast<const uint64_t*>(x), q = *static_cast<const uint64_t*>(y);
       return p < q ? -1 : p > q ? 1 : 0;
     });
-    int32_t* order = reinterpret_cast<int32_t*>(host + offset_bytes + first_bytes);
+    Piece* order = reinterpret_cast<Piece*>(host + offset_bytes + first_bytes);
     for (int64_t b = 0; b < count; ++b) {
-      order[b] = (int32_t)(uint32_t)keys[b];
+      const uint32_t graph = (uint32_t)keys[b];
       lengths[b] = (int32_t)(0xffffffffu - (uint32_t)(keys[b] >> 32));
+      order[b] = Piece{(int32_t)graph, (int32_t)offsets[graph], lengths[b], 0};
     }
     free(keys);
     memcpy(host, offsets, (size_t)(count + 1) * sizeof(int64_t));
@@ -541,7 +542,7 @@ dg_status_t dg_graph_set_batch(dg_graph_t g, int64_t count, const int64_t* offse
   g->batch_bytes = memory ? bytes : 0;
   g->batch_offsets = reinterpret_cast<const int64_t*>(memory);
   g->batch_first = memory ? reinterpret_cast<const int32_t*>(memory + offset_bytes) : nullptr;
-  g->batch_order = memory ? reinterpret_cast<const int32_t*>(memory + offset_bytes + first_bytes) : nullptr;
+  g->batch_order = memory ? reinterpret_cast<const Piece*>(memory + offset_bytes + first_bytes) : nullptr;
   g->batch_pieces = memory ? reinterpret_cast<const Piece*>(memory + offset_bytes + first_bytes + order_bytes) : nullptr;
   free(g->batch_lengths);
   g->batch_lengths = lengths;

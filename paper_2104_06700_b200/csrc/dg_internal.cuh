@@ -99,7 +99,7 @@ struct dg_graph {
   const dg::Piece* batch_pieces = nullptr;  // device: the graphs cut into runs of rows, in order
   const int32_t* batch_first = nullptr;     // device, batch_count + 1: the first piece of every graph
   int32_t batch_piece_count = 0;
-  const int32_t* batch_order = nullptr;     // device, batch_count: the graphs, longest first
+  const dg::Piece* batch_order = nullptr;   // device, batch_count: the graphs whole, longest first
   int32_t* batch_lengths = nullptr;         // host, malloc'ed: their rows
   int64_t batch_count = 1;
   int64_t batch_rows = -1;       // behind the last graph's last row; -1: n

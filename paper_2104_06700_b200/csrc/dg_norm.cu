@@ -524,17 +524,19 @@ GraphPlan graph_plan(const Graph* g, const NormArgs& a, int vec, int x_bytes, in
     plan.blocks = plan.long_blocks = (int32_t)(a.graphs * first.tiles << kClusterLog);
     return plan;
   }
-  // Many: those of more than two times what a block keeps in narrow tiles, the others as wide as an average graph leaves
-  // threads with rows.  2048 graphs of 1 to 2500 rows of 128: TIME
+  // Many: those of more than eight times what a block keeps in narrow tiles, the others as wide as an average graph leaves
+  // threads with rows.  2048 graphs of 1 to 2500 rows of 128, forward / backward: 32 / 56 us; narrow from twice what a block
+  // keeps on 33 / 58, from once 38 / 65; the long ones by clusters 43 / 74, in pieces as the long graphs' kernels take them
+  // 52 / 107.
   first = shape(narrow(64));
   if (longest > 16 * kept(first)) return none;
   across = first.across;
   while (across + least <= vectors && across + least <= kGraphThreads &&
-         2 * (int64_t)(kGraphThreads / (across + least)) * rows_kept * a.graphs >= a.rows)
+         4 * (int64_t)(kGraphThreads / (across + least)) * rows_kept * a.graphs >= a.rows)
     across += least;
   plan.shape[1] = shape(across);
   if (g->batch_lengths) {
-    const int64_t most = 2 * kept(plan.shape[1]);
+    const int64_t most = 8 * kept(plan.shape[1]);
     int64_t lo = 0, hi = a.graphs;
     while (lo < hi) {
       const int64_t mid = (lo + hi) / 2;

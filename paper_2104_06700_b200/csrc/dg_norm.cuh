@@ -432,7 +432,7 @@ __device__ __forceinline__ double block_sum(double v) { return block_sums(v, 0.0
 // there are read once.
 constexpr int kClusterLog = 3;
 // Of a block: with as few as 16 rows for a thread what a thread costs beside them counts (2048 graphs of 1 to 2500 rows of
-// 128, forward: 41 us with 256 threads, TIME with 128).
+// 128, forward: 41 us with 256 threads, 38 with 128).
 constexpr int kGraphThreads = 128;
 constexpr int kTileGroups = 128;  // most groups of a tile
 struct GraphShape {
@@ -445,7 +445,7 @@ struct GraphShape {
 // narrow ones by clusters.
 struct GraphPlan {
   GraphShape shape[2];     // of long graphs, of the others
-  const int32_t* order;    // graphs, longest first; null: one graph
+  const Piece* order;      // whole graphs, longest first; null: one graph
   int64_t blocks;          // 0: not a call for these kernels
   int32_t long_blocks, long_graphs;
   int32_t cluster_log;     // log2 of the blocks of a cluster
@@ -467,9 +467,10 @@ __device__ __forceinline__ GraphPlace graph_place(const NormArgs& a, const Graph
   const uint32_t item = (is_long ? blockIdx.x : blockIdx.x - plan.long_blocks) >> plan.cluster_log;
   r.rank = blockIdx.x & ((1 << plan.cluster_log) - 1);
   const int32_t at = item / (uint32_t)sh.tiles, tile = item - at * sh.tiles;
-  r.graph = plan.order ? plan.order[is_long ? at : at + plan.long_graphs] : 0;
-  const Rows rows = rows_of(a, r.graph);
-  r.rows = (int32_t)(rows.hi - rows.lo);
+  Piece whole{0, 0, (int32_t)a.rows, 0};
+  if (plan.order) whole = plan.order[is_long ? at : at + plan.long_graphs];
+  r.graph = whole.graph;
+  r.rows = whole.rows;
   r.tile_first = tile * sh.across * sh.vec;
   r.tile_channels = min(sh.across * sh.vec, a.F - r.tile_first);
   r.y = threadIdx.x * sh.by_across >> 16;
@@ -477,7 +478,7 @@ __device__ __forceinline__ GraphPlace graph_place(const NormArgs& a, const Graph
   r.channel = r.y < sh.down && r.x * sh.vec < r.tile_channels ? r.tile_first + r.x * sh.vec : a.F;
   r.row = r.rank * sh.down + r.y;
   r.step = sh.down << plan.cluster_log;
-  r.base = (rows.lo + r.row) * a.F + r.channel;
+  r.base = ((int64_t)whole.row + r.row) * a.F + r.channel;
   return r;
 }
 // The group of a channel of the tile: at most 2048 channels, so that the product is off by less than 1 / (2 width).
