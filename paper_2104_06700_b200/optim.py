@@ -92,7 +92,7 @@ class AdamW(torch.optim.Optimizer):
 
     def _table(self, at: int, group, first: int):
         """(gradients, the library's list) of the group's parameters that have one; the random bits of the i-th go by first + i.
-        The list is made anew when any of its parameters or states is another tensor than in the last step."""
+        The list is made anew when any of its parameters or states is another tensor, or lies elsewhere, than in the last step."""
         ids, params = range(first, first + len(group["params"])), group["params"]
         grads = [p.grad for p in params]
         if any(map(operator.is_, grads, _NONE)):
@@ -118,15 +118,15 @@ class AdamW(torch.optim.Optimizer):
             copies = [None if m is None else p for p, m in zip(params, masters)]
         else:
             targets = params
+        places = list(map(binding._data_ptr, itertools.chain(*columns[:3], [t for t in columns[3] if t is not None])))
         known = self._tables.get(at)
-        same = known is not None and len(known[0]) == len(params) and all(map(operator.is_, known[0], params)) and all(
-            all(map(operator.is_, k, c)) for k, c in zip(known[1], columns))
+        same = known is not None and known[2] == places and len(known[0]) == len(params) and all(
+            map(operator.is_, known[0], params)) and all(all(map(operator.is_, k, c)) for k, c in zip(known[1], columns))
         if same:
-            known[2].refresh(grads, targets, copies)
+            known[3].refresh(grads, targets, copies)
         else:
-            table = binding.AdamwList(grads, targets, *columns, copies, ids)
-            known = self._tables[at] = (list(params), columns, table)
-        return grads, known[2]
+            known = self._tables[at] = (list(params), columns, places, binding.AdamwList(grads, targets, *columns, copies, ids))
+        return grads, known[3]
 
     @torch.no_grad()
     def step(self, closure=None):

@@ -341,6 +341,42 @@ def test_a_captured_step_counts_on(bits):
     assert torch.equal(oa.grad_norm, ob.grad_norm)
 
 
+def test_states_and_parameters_that_move():
+    """Between steps: a state replaced, a state's memory exchanged, a parameter's memory exchanged, a gradient left out."""
+    a, b = model_params(4), model_params(4)
+    oa, ob = (optim.AdamW(ps, lr=1e-2, state_bits=8, min_8bit_size=100, max_norm=1.0) for ps in (a, b))
+
+    def both_step(k, without=None):
+        for ps in (a, b):
+            set_grads(ps, k)
+            if without is not None:
+                ps[without].grad = None
+        oa.step(), ob.step()
+
+    both_step(0)
+    kept = []
+    for change in range(4):
+        s = oa.state[a[0]]
+        if change == 0:
+            s["exp_avg"] = s["exp_avg"].clone()
+        elif change == 1:
+            kept.append(s["exp_avg_sq"].data)
+            s["exp_avg_sq"].data = s["exp_avg_sq"].data.clone()
+            kept[-1].view(torch.uint8).zero_()          # what the old memory holds does not matter any more
+        elif change == 2:
+            a[0].data = a[0].data.clone()
+        both_step(1 + change, without=1 if change == 3 else None)
+    both_step(9)
+    for p, q in zip(a, b):
+        assert torch.equal(p, q)
+        for k, t in oa.state[p].items():
+            assert torch.equal(t.float(), ob.state[q][k].float()), k
+    a[0].data = a[0].data[:, :50].contiguous()          # no longer what its states belong to
+    a[0].grad = torch.zeros_like(a[0])
+    with pytest.raises(ValueError):
+        oa.step()
+
+
 def test_refusals_and_odd_gradients():
     p = torch.nn.Parameter(torch.randn(64, 32, device=DEV))
     q = torch.nn.Parameter(p.detach().clone())
