@@ -156,7 +156,7 @@ def _has(t: Optional[torch.Tensor], count: int, name: str) -> None:
 
 # for whole lists, by map: a long list of tensors is asked in one loop
 _data_ptr, _numel, _contiguous = torch.Tensor.data_ptr, torch.Tensor.numel, torch.Tensor.is_contiguous
-_get_device, _dtype, _layout = torch.Tensor.get_device, torch.Tensor.dtype.__get__, torch.Tensor.layout.__get__
+_get_device, _dtype = torch.Tensor.get_device, torch.Tensor.dtype.__get__
 
 _TYPE_CODES = {torch.float32: DG_F32, torch.bfloat16: DG_BF16}
 

@@ -647,7 +647,7 @@ using namespace dg;
 extern "C" dg_status_t dg_grad_norm(const dg_adamw_list_t* list, float max_norm, void* workspace, float* result, void* stream) {
   if (dg_status_t st = check_list(list, workspace, true)) return st;
   if (!(max_norm >= 0.f)) return invalid("max_norm must not be negative");
-  if (!result) return invalid("result is NULL");
+  if (!result || !aligned(result, 4)) return invalid("result is NULL or misaligned");
   Workspace* ws = static_cast<Workspace*>(workspace);
   cudaStream_t s = (cudaStream_t)stream;
   int64_t at = 0;
@@ -664,6 +664,7 @@ extern "C" dg_status_t dg_adamw_step(const dg_adamw_list_t* list, double lr, dou
   if (!(beta1 >= 0.0 && beta1 < 1.0 && beta2 >= 0.0 && beta2 < 1.0)) return invalid("beta1 and beta2 must be in [0, 1)");
   if (!(lr >= 0.0 && lr < INFINITY) || !(eps >= 0.0 && eps < INFINITY) || !(weight_decay >= 0.0 && weight_decay < INFINITY))
     return invalid("lr, eps and weight_decay must be finite and not negative");
+  if (!aligned(grad_factor, 4)) return invalid("grad_factor must be aligned to its type");
   if (list->tensors == 0) return DG_OK;
   // an eps below the least normal number is that: its inverse has to be finite
   const float least = eps > 0.0 && eps < (double)kLeastScale ? kLeastScale : (float)eps;

@@ -482,6 +482,10 @@ dg_status_t dg_graph_set_batch(dg_graph_t g, int64_t count, const int64_t* offse
   if (rows < 64) rows = 64;
   int64_t pieces = 0;
   for (int64_t b = 0; b < count; ++b) pieces += (offsets[b + 1] - offsets[b] + rows - 1) / rows;
+  if (pieces >= (int64_t)1 << 31) {
+    set_error("graphs in pieces of %lld rows must be below 2^31", (long long)rows);
+    return DG_ERR_UNSUPPORTED;
+  }
   const size_t offset_bytes = align256((size_t)(count + 1) * sizeof(int64_t));
   const size_t first_bytes = align256((size_t)(count + 1) * sizeof(int32_t));
   const size_t order_bytes = align256((size_t)count * sizeof(Piece));
@@ -570,6 +574,7 @@ static dg_status_t norm_args(const Graph* g, const void* X, dg_type_t x_type, in
   if (!stats || (g->n > 0 && !X)) return invalid("a pointer is NULL");
   if ((uintptr_t)stats & 7) return invalid("stats must be 8-byte aligned");
   if ((uintptr_t)X % (x_type == DG_F32 ? 4 : 2)) return invalid("X must be aligned to its type");
+  if (((uintptr_t)weight | (uintptr_t)bias) % 4) return invalid("weight and bias must be aligned to their type");
   a->X = X;
   a->stats = reinterpret_cast<float2*>(const_cast<float*>(stats));
   a->weight = weight;
@@ -608,6 +613,7 @@ dg_status_t dg_group_norm_bwd(dg_graph_t g, const void* dY, dg_type_t y_type, co
   if ((uintptr_t)dY % y_size || (uintptr_t)dX % x_size) return invalid("dY and dX must be aligned to their types");
   if (dX && (overlaps(X, cells * x_size, dX, cells * x_size) || overlaps(dY, cells * y_size, dX, cells * x_size)))
     return invalid("the result overlaps an input");
+  if (((uintptr_t)dweight | (uintptr_t)dbias) % 4) return invalid("dweight and dbias must be aligned to their type");
   a.dY = dY;
   a.out = g->n > 0 ? dX : nullptr;
   return group_norm_bwd(g, a, x_type, y_type, act, dweight, dbias, (cudaStream_t)stream);

@@ -105,9 +105,9 @@ class AdamW(torch.optim.Optimizer):
             for p, s in zip(params, states):
                 if not s:
                     s.update(self._new_state(p, group))
-        if not {torch.strided}.issuperset(map(binding._layout, grads)):
-            raise ValueError("sparse gradients are not supported")
-        if not all(map(binding._contiguous, grads)):
+        if not all(map(binding._contiguous, grads)):     # sparse ones are not either
+            if any(g.layout is not torch.strided for g in grads):
+                raise ValueError("sparse gradients are not supported")
             grads = [g.contiguous() for g in grads]      # copies live until the launch, then the allocator's stream order serves
         columns = [[s["exp_avg"] for s in states], [s["exp_avg_sq"] for s in states], [s["step"] for s in states],
                    [s.get("scales") for s in states]]

@@ -70,6 +70,10 @@ def test_lists_that_are_refused(fake):
         assert step(fake, tensor(fake), ws=workspace(fake, shift)) == BAD
         assert norm(fake, tensor(fake), ws=workspace(fake, shift)) == BAD
     assert norm(fake, tensor(fake), result=False) == BAD
+    odd = ctypes.c_void_p(fake.array(4).value + 2)
+    assert fake.lib.dg_grad_norm(listed(fake, [tensor(fake)]), f32(1), workspace(fake), odd, None) == BAD
+    assert fake.lib.dg_adamw_step(listed(fake, [tensor(fake)]), f64(0), f64(0), f64(0), f64(0), f64(0), odd, ctypes.c_uint64(1),
+                                  workspace(fake), None) == BAD
     assert norm(fake, tensor(fake), max_norm=-1.0) == norm(fake, tensor(fake), max_norm=float("nan")) == BAD
 
 

@@ -394,6 +394,10 @@ def test_refusals_and_odd_gradients():
         bad.grad = torch.zeros_like(bad)
         with pytest.raises((ValueError, TypeError)):
             optim.AdamW([bad]).step()
+    r = torch.nn.Parameter(torch.randn(8, 8, device=DEV))
+    r.grad = torch.eye(8, device=DEV).to_sparse()
+    with pytest.raises(ValueError, match="sparse"):
+        optim.AdamW([r]).step()
     side = torch.cuda.Stream()
     side.wait_stream(torch.cuda.current_stream())
     with torch.cuda.stream(side):

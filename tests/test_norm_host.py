@@ -35,12 +35,13 @@ def test_batches_that_are_refused(fake):
 def calls(fake, g, F=12, groups=4, x_type=0, y_type=0, act=1, eps=1e-5, **moved):
     n = 64
     p = {k: fake.array(n, F) for k in ("X", "Y", "dY", "dX")}
+    p.update(dweight=fake.array(F), dbias=fake.array(F))
     p.update(weight=fake.array(F), bias=fake.array(F), stats=ctypes.c_void_p((fake.array(4 * F).value + 7) // 8 * 8))
     p.update(moved)
     fwd = fake.lib.dg_group_norm_fwd(g, p["X"], x_type, F, groups, p["weight"], p["bias"], f32(eps), act, p["Y"], y_type,
                                      p["stats"], None)
     bwd = fake.lib.dg_group_norm_bwd(g, p["dY"], y_type, p["X"], x_type, F, groups, p["weight"], p["bias"], p["stats"], act,
-                                     p["dX"], fake.array(F), fake.array(F), None)
+                                     p["dX"], p["dweight"], p["dbias"], None)
     return fwd, bwd
 
 
@@ -67,6 +68,9 @@ def test_arguments_that_are_refused(fake):
         odd = ctypes.c_void_p(fake.array(65, 12).value + 2)
         got = calls(fake, g, **{name: odd})
         assert got == ((bad if name in "XY" else ok), (ok if name == "Y" else bad)), name
+    for name in ("weight", "bias", "dweight", "dbias"):
+        odd = ctypes.c_void_p(fake.array(20).value + 2)
+        assert calls(fake, g, **{name: odd}) == (ok if name[0] == "d" else bad, bad), name
     assert calls(fake, None) == (bad, bad)
     fake.lib.dg_graph_destroy(g)
 
