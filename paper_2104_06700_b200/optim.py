@@ -1,4 +1,4 @@
-"""AdamW over all parameters in one launch, its states in 32 or 8 bits, with clipping by the norm of all gradients
+"""AdamW over all parameters, a launch for those of one kind, its states in 32 or 8 bits, with clipping by the norm of all gradients
 (dg_adamw_step and dg_grad_norm), behind torch's optimiser interface."""
 from __future__ import annotations
 
@@ -12,6 +12,23 @@ from . import binding
 
 
 _NONE = itertools.repeat(None)
+
+
+class _Table:
+    """The library's list of a group's parameters, with what it was made of."""
+
+    def __init__(self, params, states, entries, grads, ids):
+        self.params, self.states, self.entries = list(params), states, entries
+        columns = [[s["exp_avg"] for s in states], [s["exp_avg_sq"] for s in states], [s["step"] for s in states],
+                   [s.get("scales") for s in states]]
+        masters = [s.get("master") for s in states]
+        self.targets, self.copies = self.params, None
+        if not all(map(operator.is_, masters, _NONE)):
+            self.targets = [p if m is None else m for p, m in zip(params, masters)]
+            self.copies = [None if m is None else p for p, m in zip(params, masters)]
+        self.tensors = [t for column in columns for t in column if t is not None]
+        self.places = list(map(binding._data_ptr, self.tensors))
+        self.list = binding.AdamwList(grads, self.targets, *columns, self.copies, ids)
 
 
 class AdamW(torch.optim.Optimizer):
@@ -42,7 +59,7 @@ class AdamW(torch.optim.Optimizer):
             raise ValueError(f"betas must be in [0, 1), got {betas}")
         self.max_norm, self.grad_norm = max_norm, None
         self._workspace = self._result = None
-        self._tables = {}
+        self._tables, self._known_state, self._standing = {}, None, False
         super().__init__(params, dict(lr=lr, betas=betas, eps=eps, weight_decay=weight_decay, state_bits=state_bits,
                                       min_8bit_size=min_8bit_size, master_weights=master_weights, seed=seed))
 
@@ -51,7 +68,7 @@ class AdamW(torch.optim.Optimizer):
         params = self.param_groups[-1]["params"]
         if len(set(params)) != len(params):
             self.param_groups.pop()
-            raise ValueError("a parameter stands in its group twice: the one launch would update it twice at once")
+            raise ValueError("a parameter stands in its group twice: one launch would update it twice at once")
 
     def __getstate__(self):     # workspaces are not state
         state = super().__getstate__()
@@ -61,7 +78,7 @@ class AdamW(torch.optim.Optimizer):
         super().__setstate__(state)
         self.__dict__.setdefault("max_norm", None)
         self.grad_norm = self._workspace = self._result = None
-        self._tables = {}
+        self._tables, self._known_state, self._standing = {}, None, False
 
     def load_state_dict(self, state_dict) -> None:
         """torch's would cast every state to its parameter's type."""
@@ -100,33 +117,29 @@ class AdamW(torch.optim.Optimizer):
             if not some:
                 return None
             ids, params, grads = zip(*some)
-        states = [self.state[p] for p in params]
-        if not all(states):
-            for p, s in zip(params, states):
-                if not s:
-                    s.update(self._new_state(p, group))
+        known = self._tables.get(at)
+        same = self._standing and known is not None and len(known.params) == len(params) and all(
+            map(operator.is_, known.params, params))
+        states = known.states if same else [self.state[p] for p in params]
+        entries = list(itertools.chain.from_iterable(map(dict.values, states)))
+        same = same and len(entries) == len(known.entries) and all(map(operator.is_, entries, known.entries)) and \
+            list(map(binding._data_ptr, known.tensors)) == known.places
+        if not same:
+            known = None
+            if not all(states):
+                for p, s in zip(params, states):
+                    if not s:
+                        s.update(self._new_state(p, group))
+                entries = list(itertools.chain.from_iterable(map(dict.values, states)))
         if not all(map(binding._contiguous, grads)):     # sparse ones are not either
             if any(g.layout is not torch.strided for g in grads):
                 raise ValueError("sparse gradients are not supported")
             grads = [g.contiguous() for g in grads]      # copies live until the launch, then the allocator's stream order serves
-        columns = [[s["exp_avg"] for s in states], [s["exp_avg_sq"] for s in states], [s["step"] for s in states],
-                   [s.get("scales") for s in states]]
-        masters = [s.get("master") for s in states]
-        copies = None
-        if not all(map(operator.is_, masters, _NONE)):
-            targets = [p if m is None else m for p, m in zip(params, masters)]
-            copies = [None if m is None else p for p, m in zip(params, masters)]
+        if known is None:
+            known = self._tables[at] = _Table(params, states, entries, grads, ids)
         else:
-            targets = params
-        places = list(map(binding._data_ptr, itertools.chain(*columns[:3], [t for t in columns[3] if t is not None])))
-        known = self._tables.get(at)
-        same = known is not None and known[2] == places and len(known[0]) == len(params) and all(
-            map(operator.is_, known[0], params)) and all(all(map(operator.is_, k, c)) for k, c in zip(known[1], columns))
-        if same:
-            known[3].refresh(grads, targets, copies)
-        else:
-            known = self._tables[at] = (list(params), columns, places, binding.AdamwList(grads, targets, *columns, copies, ids))
-        return grads, known[3]
+            known.list.refresh(grads, known.targets, known.copies)
+        return grads, known.list
 
     @torch.no_grad()
     def step(self, closure=None):
@@ -147,6 +160,10 @@ class AdamW(torch.optim.Optimizer):
         return loss
 
     def _launch(self, device) -> None:
+        state = list(self.state), list(self.state.values())
+        self._standing = self._known_state is not None and all(
+            len(known) == len(now) and all(map(operator.is_, known, now)) for known, now in zip(self._known_state, state))
+        self._known_state = state
         parts, first = [], 0
         for at, group in enumerate(self.param_groups):
             table = self._table(at, group, first)
