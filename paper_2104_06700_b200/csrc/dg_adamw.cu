@@ -19,11 +19,13 @@ namespace {
 constexpr int kThreads = 256;
 constexpr int kWarps = kThreads / 32;
 // Blocks of an SM.  Numbers in 32 bits: two, whose 128 registers a thread hold a task's first block while the powers of beta
-// are on their way (245 M numbers: 1042 us, three blocks 1100).  In 8 bits arithmetic counts, and more warps hide it: four
-// at 64 registers (698 us; three 715, two 806, two that load a block ahead 743).
+// are on their way (245 M numbers, clipped: 1204 us, three blocks 1260).  In 8 bits arithmetic counts, and more warps hide it:
+// four at 64 registers, of which up to 19 are spilled (245 M numbers: 699 us; three blocks 760).
 constexpr int blocks_per_sm(bool eight) { return eight ? 4 : 2; }
 constexpr int kNumbers = 256;                       // of a warp's task: 8 a lane, and one scale
-constexpr int kBlocksPerTask = 4;
+// 256 numbers each, of a warp's task.  8-bit states: see step_kind (245 M numbers 718 -> 705 us against four, 120 tensors of
+// 37 M 137 -> 130).
+constexpr int kBlocksPerTask = 4, kMostBlocks = 16;
 constexpr int kNormNumbers = 2048;                  // of a warp's task of the norm
 constexpr int kNormBlocks = 148 * 4;
 constexpr float kLargest = 448.f;                   // of e4m3
@@ -128,6 +130,17 @@ __device__ __forceinline__ void store4(uint16_t* p, int left, const uint32_t* in
       if (j < left) p[j] = (uint16_t)in[j];
   }
 }
+// the upper halves of four words
+template <bool VEC>
+__device__ __forceinline__ void store_upper4(uint16_t* p, int left, const uint32_t* in) {
+  if constexpr (VEC) {
+    *reinterpret_cast<uint2*>(p) = make_uint2(__byte_perm(in[0], in[1], 0x7632), __byte_perm(in[2], in[3], 0x7632));
+  } else {
+#pragma unroll
+    for (int j = 0; j < 4; ++j)
+      if (j < left) p[j] = (uint16_t)(in[j] >> 16);
+  }
+}
 template <bool VEC>
 __device__ __forceinline__ uint32_t load_bytes(const uint8_t* p, int left) {
   if constexpr (VEC) return *reinterpret_cast<const uint32_t*>(p);
@@ -160,18 +173,15 @@ __device__ __forceinline__ Two from_e4m3(uint32_t codes) {
 
 // An 8-bit state is rounded up with a probability that is its distance from the lower neighbour: the averages move by a
 // thousandth of themselves a step, far less than half a step of 3 bits, and rounding to nearest would hold them where they
-// are.  `in_front`: the number times 2^-120, at most 448 of them up to a rounding: it has e4m3's bits in front, denormal
-// ones too, and 20 behind them; adding 16 random bits `r` there carries into them.
-__device__ __forceinline__ uint32_t to_e4m3(float in_front, uint32_t r) {
-  const uint32_t code = (__float_as_uint(in_front) + (r << 4) + 8u) >> 20;
-  return min(code, 126u);
+// are.  `in_front`: the number times 2^-120, at most 448 of them up to a rounding: behind its sign and four zeros it has e4m3's
+// bits, denormal ones too, and 20 behind them; adding 16 random bits (and half of the last) there carries into them.  The
+// code's seven bits come out in front of byte 3, over what is left of the sum: the shift by four drops the sign.
+__device__ __forceinline__ uint32_t to_e4m3(float in_front, uint32_t random_over_128) {
+  return min((__float_as_uint(in_front) << 4) + random_over_128, 0x7effffffu);
 }
-
-// A bf16 parameter is rounded up or down by 16 random bits too: steps of a thousandth of it would all be lost to nearest.
-__device__ __forceinline__ uint32_t to_bf16_random(float p, uint32_t r) {
-  const uint32_t bits = __float_as_uint(p);
-  if ((bits & 0x7f800000u) == 0x7f800000u) return __bfloat16_as_ushort(__float2bfloat16_rn(p));
-  return (bits + (r & 0xffffu)) >> 16;
+// bytes 3 of four words
+__device__ __forceinline__ uint32_t first_bytes(const uint32_t (&w)[4]) {
+  return __byte_perm(__byte_perm(w[0], w[1], 0x0073), __byte_perm(w[2], w[3], 0x0073), 0x5410);
 }
 
 // 1 / v, off by at most 2^-23 of itself
@@ -180,10 +190,10 @@ __device__ __forceinline__ float fast_inverse(float v) {
   asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(v));
   return r;
 }
-// The larger magnitude, NaN if one is.
-__device__ __forceinline__ float most_of(float a, float b) {
+// The largest magnitude, NaN if one is.
+__device__ __forceinline__ float most_of(float a, float b, float c) {
   float r;
-  asm("max.NaN.f32 %0, %1, %2;" : "=f"(r) : "f"(a), "f"(fabsf(b)));
+  asm("max.NaN.abs.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(a), "f"(b), "f"(c));
   return r;
 }
 __device__ __forceinline__ float warp_most(float v) {
@@ -215,9 +225,15 @@ __device__ __forceinline__ void store_param(const Tensors<N>& a, int i, int64_t 
       store4<VEC>(reinterpret_cast<uint16_t*>(a.copy[i]) + q, left, c);
     }
   } else {
+    // Rounded up or down by 16 random bits too: steps of a thousandth of a parameter would all be lost to nearest.
 #pragma unroll
-    for (int j = 0; j < 4; ++j) c[j] = to_bf16_random(p[j], r[j]);
-    store4<VEC>(static_cast<uint16_t*>(a.param[i]) + q, left, c);
+    for (int j = 0; j < 4; ++j) c[j] = __float_as_uint(p[j]) + (r[j] & 0xffffu);
+    if (!(most_of(most_of(p[0], p[1], p[2]), p[3], 0.f) < INFINITY)) {
+#pragma unroll
+      for (int j = 0; j < 4; ++j)
+        if (!(fabsf(p[j]) < INFINITY)) c[j] = (uint32_t)__bfloat16_as_ushort(__float2bfloat16_rn(p[j])) << 16;
+    }
+    store_upper4<VEC>(static_cast<uint16_t*>(a.param[i]) + q, left, c);
   }
 }
 
@@ -290,8 +306,8 @@ __device__ __forceinline__ void update(const Tensors<N>& a, int i, int64_t base,
       const float2 pj = apart(fma2(ratio, both(-st.c1), two(p[2 * j], p[2 * j + 1]) * both(h.decay)));
       p[2 * j] = pj.x, p[2 * j + 1] = pj.y;
       m[2 * j] = mj.x, m[2 * j + 1] = mj.y;
-      most_m = most_of(most_of(most_m, mj.x), mj.y);
-      most_u = most_of(most_of(most_u, v[2 * j]), v[2 * j + 1]);
+      most_m = most_of(most_m, mj.x, mj.y);
+      most_u = most_of(most_u, v[2 * j], v[2 * j + 1]);
     }
     most_m = warp_most(most_m);
     most_u = warp_most(most_u);
@@ -318,20 +334,24 @@ __device__ __forceinline__ void update(const Tensors<N>& a, int i, int64_t base,
       uint32_t r[4], cm[4], cu[4];
 #pragma unroll
       for (int j = 0; j < 4; ++j) {
-        const float mj = m[4 * k + j], uj = v[4 * k + j];
         r[j] = mix((uint32_t)(q + j) + key);
-        cm[j] = to_e4m3(fabsf(ym[4 * k + j]), r[j] & 0xffff);
-        cu[j] = to_e4m3(yu[4 * k + j], r[j] >> 16);
-        cu[j] = max(cu[j], min(__float_as_uint(uj), 1u));  // a denominator that was not 0 does not become 0
-        if (careful) {
-          if (!(fabsf(mj) < INFINITY)) cm[j] = 0x7f;
-          if (!(uj < INFINITY)) cu[j] = 0x7f;
-        }
-        cm[j] |= __float_as_uint(mj) >> 24 & 0x80u;
+        cm[j] = to_e4m3(ym[4 * k + j], __byte_perm(r[j], 0x80u, 0x5104));
+        cu[j] = to_e4m3(yu[4 * k + j], __byte_perm(r[j], 0x80u, 0x5324));
+        // a denominator that was not 0 does not become 0 (a root that is not 0 is above 2^-75)
+        cu[j] = max(cu[j], min(__float_as_uint(v[4 * k + j]), 0x01000000u));
       }
+      if (careful) {
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          if (!(fabsf(m[4 * k + j]) < INFINITY)) cm[j] = 0x7f000000u;
+          if (!(v[4 * k + j] < INFINITY)) cu[j] = 0x7f000000u;
+        }
+      }
+#pragma unroll
+      for (int j = 0; j < 4; ++j) cm[j] |= __float_as_uint(m[4 * k + j]) & 0x80000000u;
       store_param<P, VEC>(a, i, q, left, p + 4 * k, r);
-      store_bytes<VEC>(static_cast<uint8_t*>(a.m[i]) + q, left, __byte_perm(__byte_perm(cm[0], cm[1], 0x0040), __byte_perm(cm[2], cm[3], 0x0040), 0x5410));
-      store_bytes<VEC>(static_cast<uint8_t*>(a.v[i]) + q, left, __byte_perm(__byte_perm(cu[0], cu[1], 0x0040), __byte_perm(cu[2], cu[3], 0x0040), 0x5410));
+      store_bytes<VEC>(static_cast<uint8_t*>(a.m[i]) + q, left, first_bytes(cm));
+      store_bytes<VEC>(static_cast<uint8_t*>(a.v[i]) + q, left, first_bytes(cu));
     }
   } else {
 #pragma unroll
@@ -562,7 +582,15 @@ dg_status_t step_kind(const dg_adamw_list_t& t, int kind, const StepCall& c) {
     if (a.n == 0) break;
     const int64_t warps = (int64_t)c.sms * blocks_per_sm(EIGHT) * kWarps;
     // Long tasks where every warp has some: what a warp finds out about its tensor serves more numbers.
-    if (tasks > warps * 2 * kBlocksPerTask) tasks = fill(t, &(at = from), kind, kNumbers * kBlocksPerTask, &a);
+    if (EIGHT && tasks > warps) {
+      // of so many blocks that a few whole rounds of the warps take them all; a tensor's last task is half empty on average
+      const int64_t rounds = (tasks + warps * kMostBlocks - 1) / (warps * kMostBlocks), half_empty = a.n / 2;
+      const int64_t places = warps * rounds > 2 * half_empty ? warps * rounds - half_empty : half_empty + 1;
+      const int64_t each = (tasks + places - 1) / places;
+      tasks = fill(t, &(at = from), kind, kNumbers * (int32_t)each, &a);
+    } else if (!EIGHT && tasks > warps * 2 * kBlocksPerTask) {
+      tasks = fill(t, &(at = from), kind, kNumbers * kBlocksPerTask, &a);
+    }
     int64_t blocks = (tasks + kWarps - 1) / kWarps;
     if (blocks > c.sms * blocks_per_sm(EIGHT)) blocks = c.sms * blocks_per_sm(EIGHT);
     if (blocks < 1) blocks = 1;  // tensors without numbers count their steps too

@@ -139,6 +139,31 @@ def test_lists_longer_than_a_launch(count):
     assert not bool(workspace[:8].any())       # the tickets are back at 0
 
 
+@pytest.mark.parametrize("p_type,bits,sizes", [(F32, 8, [5000011, 257, 1300001, 700000]), (BF16, 8, [1300001, 4096]),
+                                               (BF16, 8, [40000 + i for i in range(60)]), (F32, 32, [10000007, 300])])
+def test_more_numbers_than_warps_have_in_one_go(p_type, bits, sizes):
+    tensors = [Tensor(n, p_type, p_type, bits, i, taken=i) for i, n in enumerate(sizes)]
+    before = [t.snapshot() for t in tensors]
+    step(tensors, seed=9)
+    for t, b in zip(tensors, before):
+        t.check(b, seed=9)
+
+
+@pytest.mark.parametrize("bits", [32, 8])
+def test_bf16_parameters_that_are_not_finite_keep_to_themselves(bits):
+    t, clean = (Tensor(1000, BF16, BF16, bits, 4) for _ in range(2))
+    t.p[[5, 700]], t.p[[300, 999]] = float("nan"), float("-inf")
+    before = clean.snapshot()
+    step([t])
+    step([clean])
+    clean.check(before)
+    assert t.p[[5, 700]].isnan().all() and t.p[[300, 999]].tolist() == [-float("inf")] * 2
+    rest = torch.ones(1000, dtype=torch.bool, device=DEV)
+    rest[[5, 700, 300, 999]] = False
+    assert torch.equal(t.p[rest], clean.p[rest])
+    assert torch.equal(t.m.float(), clean.m.float()) and torch.equal(t.v.float(), clean.v.float())
+
+
 @pytest.mark.parametrize("sizes,types", [([1], F32), ([5, 0, 256, 70001], F32), ([33, 1000003], BF16)])
 def test_norm_of_gradients(sizes, types):
     gen = torch.Generator(device=DEV).manual_seed(1)
