@@ -402,6 +402,34 @@ def test_states_and_parameters_that_move():
         oa.step()
 
 
+def test_state_dictionaries_that_are_exchanged():
+    """Between steps: one parameter's dictionary replaced by a copy, then taken out (it begins anew), a group added."""
+    gen = torch.Generator(device=DEV).manual_seed(3)
+    start = [torch.randn(n, device=DEV, generator=gen) for n in (700, 700, 33)]
+    grads = [[torch.randn(p.numel(), device=DEV, generator=gen) for p in start] for _ in range(5)]
+    params = [torch.nn.Parameter(p.clone()) for p in start]
+    alone = [torch.nn.Parameter(p.clone()) for p in start]
+    together = optim.AdamW(params[:2], lr=1e-2)
+    single = [optim.AdamW([p], lr=1e-2) for p in alone]
+    for k in range(5):
+        if k == 1:
+            old = together.state[params[0]]
+            together.state[params[0]] = {key: t.clone() for key, t in old.items()}
+            for t in old.values():
+                t.fill_(7)
+        elif k == 2:
+            del together.state[params[1]]
+            single[1] = optim.AdamW([alone[1]], lr=1e-2)
+        elif k == 3:
+            together.add_param_group(dict(params=params[2:]))
+        for i in range(3 if k >= 3 else 2):
+            params[i].grad, alone[i].grad = grads[k][i], grads[k][i].clone()
+            single[i].step()
+        together.step()
+        for p, q in zip(params, alone):
+            assert torch.equal(p, q), k
+
+
 def test_refusals_and_odd_gradients():
     p = torch.nn.Parameter(torch.randn(64, 32, device=DEV))
     q = torch.nn.Parameter(p.detach().clone())
