@@ -489,6 +489,9 @@ GraphPlan graph_plan(const Graph* g, const NormArgs& a, int vec, int x_bytes, in
   while (least % vec) least += a.width;
   least /= vec;
   if (least > kGraphThreads) return none;
+  // The most: threads of a block, and groups that its arrays hold.  (The fewest hold no more groups than a vector channels.)
+  int32_t most = vectors < kGraphThreads ? vectors : kGraphThreads;
+  if (most > kTileGroups * a.width / vec) most = kTileGroups * a.width / vec;
   plan.by_width = 1.f / a.width;
   plan.order = g->batch_order;
   auto shape = [&](int32_t across) {
@@ -508,7 +511,7 @@ GraphPlan graph_plan(const Graph* g, const NormArgs& a, int vec, int x_bytes, in
   };
   auto narrow = [&](int bytes) {
     int32_t across = least;
-    while (across * vec * x_bytes < bytes && across + least <= vectors && across + least <= kGraphThreads) across += least;
+    while (across * vec * x_bytes < bytes && across + least <= most) across += least;
     return across;
   };
   auto kept = [&](const GraphShape& sh) { return (int64_t)sh.down * rows_kept; };  // rows in a block's shared memory
@@ -531,8 +534,7 @@ GraphPlan graph_plan(const Graph* g, const NormArgs& a, int vec, int x_bytes, in
   first = shape(narrow(64));
   if (longest > 16 * kept(first)) return none;
   across = first.across;
-  while (across + least <= vectors && across + least <= kGraphThreads &&
-         4 * (int64_t)(kGraphThreads / (across + least)) * rows_kept * a.graphs >= a.rows)
+  while (across + least <= most && 4 * (int64_t)(kGraphThreads / (across + least)) * rows_kept * a.graphs >= a.rows)
     across += least;
   plan.shape[1] = shape(across);
   if (g->batch_lengths) {
