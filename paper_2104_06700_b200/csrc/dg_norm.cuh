@@ -65,13 +65,14 @@ __device__ __forceinline__ float activated(float z) {
   return z;
 }
 // Of a pair of numbers not below -43 (see above_floor), with one reciprocal for both, that of the product: hardware's
-// functions bound these kernels (2.4 M x 100 bf16, SiLU, forward: 285 us, 292 with two reciprocals).
+// functions bound these kernels (2.4 M x 100 bf16, SiLU, forward: 285 us, 292 with two reciprocals).  The pair may lie in two
+// groups: NaN is taken for -43 here, so that it does not reach the other one through the product.  The caller's z is NaN still.
 __device__ __forceinline__ Two sigmoid(Two z) {
   const float2 t = apart(z * both(-1.4426950408889634f));
   float2 e;
   float r;
-  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(e.x) : "f"(t.x));
-  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(e.y) : "f"(t.y));
+  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(e.x) : "f"(fminf(t.x, 63.f)));  // at most 62.04, or NaN
+  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(e.y) : "f"(fminf(t.y, 63.f)));
   e = apart(two(e.x, e.y) + both(1.f));
   asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(e.x * e.y));
   return both(r) * two(e.y, e.x);
