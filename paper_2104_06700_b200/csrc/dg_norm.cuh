@@ -50,42 +50,50 @@ __device__ __forceinline__ T as(float v) {
 }
 
 // 1 / (1 + exp(-z)), of hardware's 2^x and 1 / x: off by 2 + |1.5 z| units of 2^-23.  A cell costs 4 to 12 bytes of memory
-// traffic, and the exact functions cost as much time.
-__device__ __forceinline__ float sigmoid(float z) {
-  float e, r;
-  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(e) : "f"(z * -1.4426950408889634f));
-  asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(1.f + e));
+// traffic, and the exact functions cost as much time.  *t: exp(-z).
+__device__ __forceinline__ float sigmoid(float z, float* t) {
+  float r;
+  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(*t) : "f"(z * -1.4426950408889634f));
+  asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(1.f + *t));
   return r;
+}
+// z, or -43 below that: SiLU and its derivative are under 10^-17 there, and the product of two 1 + exp(-z) is finite.  NaN stays.
+__device__ __forceinline__ float above_floor(float z) {
+  asm("max.NaN.f32 %0, %0, %1;" : "+f"(z) : "f"(-43.f));
+  return z;
+}
+__device__ __forceinline__ Two above_floor(Two z) {
+  const float2 q = apart(z);
+  return two(above_floor(q.x), above_floor(q.y));
 }
 
 template <int ACT>
 __device__ __forceinline__ float activated(float z) {
   if constexpr (ACT == DG_ACT_RELU) return z <= 0.f ? 0.f : z;  // NaN stays NaN
-  if constexpr (ACT == DG_ACT_SILU) return z * sigmoid(z);
+  if constexpr (ACT == DG_ACT_SILU) {
+    float t;
+    z = above_floor(z);
+    return z * sigmoid(z, &t);
+  }
   return z;
 }
-// Of a pair of numbers not below -43 (see above_floor), with one reciprocal for both, that of the product: hardware's
+// Of a pair of numbers not below -43, with one reciprocal for both, that of the product: hardware's
 // functions bound these kernels (2.4 M x 100 bf16, SiLU, forward: 285 us, 292 with two reciprocals).  The pair may lie in two
 // groups: NaN is taken for -43 here, so that it does not reach the other one through the product.  The caller's z is NaN still.
-__device__ __forceinline__ Two sigmoid(Two z) {
-  const float2 t = apart(z * both(-1.4426950408889634f));
+__device__ __forceinline__ Two sigmoid(Two z, Two* t) {
+  const float2 q = apart(z * both(-1.4426950408889634f));
   float2 e;
   float r;
-  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(e.x) : "f"(fminf(t.x, 63.f)));  // at most 62.04, or NaN
-  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(e.y) : "f"(fminf(t.y, 63.f)));
-  e = apart(two(e.x, e.y) + both(1.f));
+  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(e.x) : "f"(fminf(q.x, 63.f)));  // at most 62.04, or NaN
+  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(e.y) : "f"(fminf(q.y, 63.f)));
+  *t = two(e.x, e.y);
+  e = apart(*t + both(1.f));
   asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(e.x * e.y));
   return both(r) * two(e.y, e.x);
 }
-// z, or -43 below that: SiLU and its derivative are under 10^-17 there, and the product of two 1 + exp(-z) is finite.  NaN stays.
-__device__ __forceinline__ Two above_floor(Two z) {
-  float2 q = apart(z);
-  asm("max.NaN.f32 %0, %0, %1;" : "+f"(q.x) : "f"(-43.f));
-  asm("max.NaN.f32 %0, %0, %1;" : "+f"(q.y) : "f"(-43.f));
-  return two(q.x, q.y);
-}
 
-// dy act'(z).  The ReLU's border is where z changes its sign: near it (|hat w| is about |b| there and z is off by up to
+// dy act'(z).  SiLU' = s (1 + z (1 - s)), where 1 - s is t s with t = exp(-z): a difference would keep s's rounding, which a large z
+// multiplies (z = 10^6 beside a moderate one: 6 % off).  The ReLU's border is where z changes its sign: near it (|hat w| is about |b| there and z is off by up to
 // 2^-22 |b|) the sign is taken in 64 bits, so that no row's gradient is lost or added by rounding.
 template <int ACT>
 __device__ __forceinline__ float before_activation(float dy, float x, float mean, float rstd, float w, float b) {
@@ -96,8 +104,10 @@ __device__ __forceinline__ float before_activation(float dy, float x, float mean
     const double exact = ((double)x - mean) * rstd * w + b;
     return exact <= 0.0 ? 0.f : dy;
   }
-  const float s = sigmoid(z);
-  return dy * (s * fmaf(z, 1.f - s, 1.f));
+  const float q = above_floor(z);
+  float t;
+  const float s = sigmoid(q, &t);
+  return dy * (s * fmaf(q, t * s, 1.f));
 }
 
 // ---- rows in pieces: the kernels of long graphs ------------------------------------------------------------------
@@ -326,7 +336,8 @@ __device__ __forceinline__ void normalise(Channels<VEC>& v, const Fixed<VEC>& f)
     Two z = fma2((pair_of(v, k) - f.mean[k]) * f.rstd[k], f.w[k], f.b[k]);
     if constexpr (ACT == DG_ACT_SILU) {
       z = above_floor(z);
-      z = z * sigmoid(z);
+      Two t;
+      z = z * sigmoid(z, &t);
     }
     if constexpr (ACT == DG_ACT_RELU) {
       const float2 q = apart(z);
@@ -346,8 +357,9 @@ __device__ __forceinline__ void backward_terms(Two x, Two dy, const Fixed<VEC>& 
     Two z = fma2(*hat, f.w[k], f.b[k]);
     if constexpr (ACT == DG_ACT_SILU) {
       z = above_floor(z);
-      const Two s = sigmoid(z);
-      *d = dy * (s * fma2(z, both(1.f) - s, both(1.f)));
+      Two t;
+      const Two s = sigmoid(z, &t);
+      *d = dy * (s * fma2(z, t * s, both(1.f)));
     } else {
       const float2 zs = apart(z), ds = apart(dy), bs = apart(f.b[k]);
       float2 r = make_float2(zs.x <= 0.f ? 0.f : ds.x, zs.y <= 0.f ? 0.f : ds.y);
