@@ -306,7 +306,8 @@ class GraphSAGE(torch.nn.Module):
         for i, lin in enumerate(self.lin):
             project = self.project_first and lin.out_features < lin.in_features
             relu = i + 1 < len(self.lin) and not self.norms
-            if _is_plain(lin):
+            plain = _is_plain(lin)     # asked once: the module may take its hooks away while it runs
+            if plain:
                 width = lin.out_features if project else lin.in_features
                 H = _GcnLayer.apply(H, lin.weight, lin.bias, self.graph, self.inv_deg1, relu, project,
                                     self.bf16_aggregate and width % 2 == 0)
@@ -316,7 +317,7 @@ class GraphSAGE(torch.nn.Module):
                 H = lin(self._aggregated(H))
             if self.norms and i + 1 < len(self.lin):
                 H = self.norms[i](H, self._input_type(i + 1))
-            elif relu and not _is_plain(lin):
+            elif relu and not plain:
                 H = torch.relu(H)
         return H
 
