@@ -8,8 +8,9 @@
 namespace dg {
 namespace {
 
-// Rows a thread has in flight, and takes the mean of before it joins that to what it has.
-constexpr int kStatRows = 8;
+// Rows a thread has in flight, and most rows of a stretch: sums in 32 bits go over no more.  (All of a thread's rows in one, with
+// 1690 a thread and the first at 10^4 standard deviations: 1 / sqrt(var) 2e-4 off.)
+constexpr int kStatRows = 8, kStretch = 64;
 // Rows of a thread in shared memory: eight blocks on an SM.
 constexpr int kStep = 4, kRing = 3, kSlots = kStep * kRing;
 
@@ -95,13 +96,15 @@ __device__ __forceinline__ void join_block(float& n, Moments (&m)[UNITS], Moment
   }
 }
 
-// partial[piece][unit]: the moments of a piece's rows.  A thread sums differences from the mean of its first rows, and their
-// squares: what is lost when its own mean is taken off is of the order of those rows' distance from the others.
+// partial[piece][unit]: the moments of a piece's rows.  A thread sums differences from a number near by, and their squares, over
+// stretches of rows, and joins the stretches' moments in 64 bits.  What is lost when a stretch's own mean is taken off is of
+// the order of its rows' distance from that number: the mean of the first rows, then that of the stretch before.  The first
+// two stretches are short, so that rows far from all others in front (a hub's) do not count for many.
 template <typename X, int VEC, bool SHARED>
 __global__ void __launch_bounds__(kNormThreads, VEC == 8 ? 3 : 4)
     norm_stats_kernel(NormArgs a, NormShape sh, const Piece* pieces, float2* partial) {
   constexpr int kEach = kUnits<VEC, SHARED>, kP = kPairs<VEC>;
-  __shared__ Moments parts[kNormThreads * kEach];
+  __shared__ double2 stretches[kNormThreads * kEach];  // (mean, sum of squares about it) of the thread's stretches so far
   __shared__ float counts[kNormThreads];
   const Place at = place_of(a, sh, pieces, blockIdx.x);
   Moments m[kEach] = {};
@@ -141,42 +144,64 @@ __global__ void __launch_bounds__(kNormThreads, VEC == 8 ? 3 : 4)
 #pragma unroll
       for (int k = 0; k < kP; ++k) from[k] = pair_of(mean, k) * both(inverse);
     }
-    int32_t r = 0;
-    for (; r + kStatRows <= rows - sh.kept; r += kStatRows, x += kStatRows * pace) {
-      Channels<VEC> v[kStatRows];
+    // Joins the sums of the last `some` rows to the stretches before, which have `before`; the next begins.
+    auto close = [&](int32_t before, int32_t some) {
+      const float inverse = 1.f / (some * (SHARED ? VEC : 1));
+      const double share = (double)some / (before + some), weight = (double)before * (SHARED ? VEC : 1) * share;
+      Channels<VEC> s, q, f;
 #pragma unroll
-      for (int u = 0; u < kStatRows; ++u) v[u] = load_channels<X, VEC, true>(x + u * pace);
+      for (int k = 0; k < kP; ++k) set_pair(s, k, sum[k]), set_pair(q, k, squares[k]), set_pair(f, k, from[k]);
+#pragma unroll
+      for (int c = 0; c < kEach; ++c) {
+        float total = s.v[c], all = q.v[c];
+        if constexpr (SHARED) {
+#pragma unroll
+          for (int o = 1; o < VEC; ++o) total += s.v[o], all += q.v[o];
+        }
+        const float off = total * inverse, m2 = fmaf(-off, total, all), mean = f.v[c] + off;
+        double2* const so_far = stretches + c * kNormThreads + threadIdx.x;
+        double2 r = before > 0 ? *so_far : make_double2(0.0, 0.0);
+        const double d = mean - r.x;
+        r.x += d * share;
+        r.y += (m2 < 0.f ? 0.f : m2) + d * d * weight;  // NaN stays NaN
+        *so_far = r;
+        f.v[c] = mean;
+      }
+#pragma unroll
+      for (int k = 0; k < kP; ++k) {
+        from[k] = SHARED ? both(f.v[0]) : pair_of(f, k);
+        sum[k] = squares[k] = both(0.f);
+      }
+    };
+    int32_t r = 0, begin = 0;
+    while (r + kStatRows <= rows) {
+      Channels<VEC> v[kStatRows];
+      if (r + kStatRows <= rows - sh.kept) {
+#pragma unroll
+        for (int u = 0; u < kStatRows; ++u) v[u] = load_channels<X, VEC, true>(x + u * pace);
+      } else {
+#pragma unroll
+        for (int u = 0; u < kStatRows; ++u) v[u] = load_channels<X, VEC, false>(x + u * pace);
+      }
 #pragma unroll
       for (int u = 0; u < kStatRows; ++u) add(v[u]);
-    }
-    for (; r + kStatRows <= rows; r += kStatRows, x += kStatRows * pace) {
-      Channels<VEC> v[kStatRows];
-#pragma unroll
-      for (int u = 0; u < kStatRows; ++u) v[u] = load_channels<X, VEC, false>(x + u * pace);
-#pragma unroll
-      for (int u = 0; u < kStatRows; ++u) add(v[u]);
-    }
-    for (; r < rows; ++r, x += pace) add(load_channels<X, VEC, false>(x));
-    Channels<VEC> s, q, f;
-#pragma unroll
-    for (int k = 0; k < kP; ++k) set_pair(s, k, sum[k]), set_pair(q, k, squares[k]), set_pair(f, k, from[k]);
-    if constexpr (SHARED) {
-      n = (float)rows * VEC;
-      float total = 0.f, all = 0.f;
-#pragma unroll
-      for (int c = 0; c < VEC; ++c) total += s.v[c], all += q.v[c];
-      const float off = total / n, m2 = fmaf(-off, total, all);
-      m[0] = Moments{f.v[0] + off, m2 < 0.f ? 0.f : m2};  // NaN stays NaN
-    } else {
-      n = (float)rows;
-#pragma unroll
-      for (int c = 0; c < VEC; ++c) {
-        const float off = s.v[c] / n, m2 = fmaf(-off, s.v[c], q.v[c]);
-        m[c] = Moments{f.v[c] + off, m2 < 0.f ? 0.f : m2};  // NaN stays NaN
+      r += kStatRows, x += kStatRows * pace;
+      if (r % kStretch == 0 || r <= 2 * kStatRows) {
+        close(begin, r - begin);
+        begin = r;
       }
     }
+    for (; r < rows; ++r, x += pace) add(load_channels<X, VEC, false>(x));
+    if (r > begin) close(begin, r - begin);
+    n = (float)rows * (SHARED ? VEC : 1);
+#pragma unroll
+    for (int k = 0; k < kEach; ++k) {
+      const double2 all = stretches[k * kNormThreads + threadIdx.x];
+      m[k] = Moments{(float)all.x, (float)all.y};
+    }
   }
-  join_block<kEach>(n, m, parts, counts, sh.across, sh.down);
+  __syncthreads();  // the places are used anew
+  join_block<kEach>(n, m, reinterpret_cast<Moments*>(stretches), counts, sh.across, sh.down);
   if (at.y == 0 && at.channel < a.F) {
     const int32_t units = a.F / VEC * kEach;
     float2* out = partial + (int64_t)blockIdx.x * units + at.channel / VEC * kEach;

@@ -66,13 +66,16 @@ __device__ __forceinline__ Channels<VEC> gradient_of(const Channels<VEC>& x, con
   return r;
 }
 
-// partial[piece][channel] = (sum of d, sum of d hat).  The sums of every kRows rows are added to the thread's.
+// partial[piece][channel] = (sum of d, sum of d hat).  The sums of every kRows rows are added to the thread's in 32 bits, those
+// of kStretch times as many to its place in shared memory in 64: what is lost does not grow with the rows.
 template <typename X, typename Y, int ACT, int VEC>
 __global__ void __launch_bounds__(kNormThreads, kPieceBlocks)
     norm_sums_kernel(NormArgs a, NormShape sh, const Piece* pieces, float2* partial) {
-  __shared__ float2 parts[kNormThreads * VEC];
+  constexpr int kStretch = 16;
+  __shared__ double2 parts[kNormThreads * VEC];
   const Place at = place_of(a, sh, pieces, blockIdx.x);
-  float2 total[VEC] = {};
+#pragma unroll
+  for (int c = 0; c < VEC; ++c) parts[c * kNormThreads + threadIdx.x] = make_double2(0.0, 0.0);
   if (at.channel < a.F && at.y < at.piece.rows) {
     const Fixed<VEC> f = fixed_of<VEC>(a, at.piece.graph, at.channel);
     int32_t rows = (at.piece.rows - at.y + at.down - 1) / at.down;
@@ -80,6 +83,17 @@ __global__ void __launch_bounds__(kNormThreads, kPieceBlocks)
     const X* x = static_cast<const X*>(a.X) + base;
     const Y* dy = static_cast<const Y*>(a.dY) + base;
     Sums<ACT, VEC> all = {};
+    auto close = [&]() {
+      float2 total[VEC];
+      all.put(total);
+#pragma unroll
+      for (int c = 0; c < VEC; ++c) {
+        double2* const so_far = parts + c * kNormThreads + threadIdx.x;
+        *so_far = make_double2(so_far->x + total[c].x, so_far->y + total[c].y);
+      }
+      all = Sums<ACT, VEC>{};
+    };
+    int32_t steps = 0;
     auto step = [&](auto once) {
       constexpr bool kOnce = decltype(once)::value;
       Channels<VEC> v[kRows], d[kRows];
@@ -92,15 +106,14 @@ __global__ void __launch_bounds__(kNormThreads, kPieceBlocks)
 #pragma unroll
       for (int u = 0; u < kRows; ++u) some.add(v[u], d[u], f);
       all.add(some);
+      if (++steps % kStretch == 0) close();
       rows -= kRows, x += kRows * pace, dy += kRows * pace;
     };
     while (rows >= kRows + sh.kept) step(std::true_type());
     while (rows >= kRows) step(std::false_type());
     for (; rows > 0; --rows, x += pace, dy += pace) all.add(load_channels<X, VEC, false>(x), load_channels<Y, VEC, false>(dy), f);
-    all.put(total);
+    close();
   }
-#pragma unroll
-  for (int c = 0; c < VEC; ++c) parts[c * kNormThreads + threadIdx.x] = total[c];
   int half = 1;
   while (half < sh.down) half *= 2;
   for (half /= 2; half > 0; half /= 2) {
@@ -109,17 +122,19 @@ __global__ void __launch_bounds__(kNormThreads, kPieceBlocks)
     if (at.y < half && at.y + half < sh.down) {
 #pragma unroll
       for (int c = 0; c < VEC; ++c) {
-        const float2 o = parts[c * kNormThreads + other];
-        total[c].x += o.x;
-        total[c].y += o.y;
-        parts[c * kNormThreads + threadIdx.x] = total[c];
+        double2* const mine = parts + c * kNormThreads + threadIdx.x;
+        const double2 o = parts[c * kNormThreads + other];
+        *mine = make_double2(mine->x + o.x, mine->y + o.y);
       }
     }
   }
   if (at.y == 0 && at.channel < a.F) {
     float2* out = partial + (int64_t)blockIdx.x * a.F + at.channel;
 #pragma unroll
-    for (int c = 0; c < VEC; ++c) out[c] = total[c];
+    for (int c = 0; c < VEC; ++c) {
+      const double2 total = parts[c * kNormThreads + threadIdx.x];
+      out[c] = make_float2((float)total.x, (float)total.y);
+    }
   }
 }
 
@@ -334,27 +349,27 @@ __global__ void __launch_bounds__(kNormThreads, kPieceBlocks)
   const int32_t tile_first = blockIdx.y * sh.across * VEC, tile_end = min(tile_first + sh.across * VEC, a.F);
   const int32_t first_group = tile_first / a.width, groups = (tile_end - 1) / a.width - first_group + 1;
   const Rows graph_rows = rows_of(a, at.piece.graph);
-  const float n = (float)(graph_rows.hi - graph_rows.lo) * a.width;
+  const double n = (double)(graph_rows.hi - graph_rows.lo) * a.width;
   const float2* mine = totals + (int64_t)at.piece.graph * a.F;
   int32_t lanes = 1;
   while (lanes < a.width && lanes < 32) lanes *= 2;
   for (int32_t g0 = 0; g0 < groups; g0 += kNormThreads / lanes) {
     const int32_t g = g0 + threadIdx.x / lanes;
-    float s1 = 0.f, s2 = 0.f;
+    double s1 = 0.0, s2 = 0.0;
     if (g < groups) {
       for (int32_t k = threadIdx.x % lanes; k < a.width; k += lanes) {
         const int32_t channel = (first_group + g) * a.width + k;
         const float2 t = mine[channel];
-        const float w = a.weight ? a.weight[channel] : 1.f;
-        s1 = fmaf(w, t.x, s1);
-        s2 = fmaf(w, t.y, s2);
+        const double w = a.weight ? a.weight[channel] : 1.f;
+        s1 += w * t.x;
+        s2 += w * t.y;
       }
     }
     for (int o = lanes / 2; o > 0; o /= 2) {
       s1 += __shfl_xor_sync(0xffffffffu, s1, o);
       s2 += __shfl_xor_sync(0xffffffffu, s2, o);
     }
-    if (g < groups && threadIdx.x % lanes == 0) means[g] = make_float2(s1 / n, s2 / n);
+    if (g < groups && threadIdx.x % lanes == 0) means[g] = make_float2((float)(s1 / n), (float)(s2 / n));
   }
   __syncthreads();
   if (at.channel >= a.F || at.y >= at.piece.rows) return;
