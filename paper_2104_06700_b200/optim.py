@@ -81,8 +81,18 @@ class AdamW(torch.optim.Optimizer):
         self._tables, self._known_state, self._standing = {}, None, False
 
     def load_state_dict(self, state_dict) -> None:
-        """torch's would cast every state to its parameter's type."""
-        super().load_state_dict(state_dict)
+        """torch's would cast every state to its parameter's type.  The states are new tensors: a step captured before must not be
+        replayed afterwards."""
+        given = {}      # what the registered hooks made of it: ours comes behind the others, and before theirs when it is loaded
+        ours = [self.register_load_state_dict_pre_hook(lambda _, last: given.update(last)),
+                self.register_load_state_dict_post_hook(lambda _: self._take_states(given), prepend=True)]
+        try:
+            super().load_state_dict(state_dict)
+        finally:
+            for handle in ours:
+                handle.remove()
+
+    def _take_states(self, state_dict) -> None:
         saved = state_dict["state"]
         params = [p for group in self.param_groups for p in group["params"]]
         numbers = [i for group in state_dict["param_groups"] for i in group["params"]]
