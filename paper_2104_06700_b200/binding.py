@@ -292,6 +292,8 @@ class AdamwList:
             device = self.device
             _check_tensors(steps, {torch.int64}, device, "steps")
             _check_sizes(steps, [1] * self.count, "steps")
+            if scales is not None and len(scales) != self.count:
+                raise ValueError(f"scales must be {self.count}, got {len(scales)}")
             eight = [s is not None for s in scales] if scales is not None else [False] * self.count
             for name, tensors in (("exp_avgs", exp_avgs), ("exp_avg_sqs", exp_avg_sqs)):
                 _check_sizes(tensors, self._numbers, name)
@@ -326,6 +328,8 @@ class AdamwList:
                     self._types[at - 1] = types
                 _check_sizes(tensors, self._numbers, name)
                 fields[at] = _pointers(tensors)
+        if copies is not None and len(copies) != self.count:
+            raise ValueError(f"copies must be {self.count}, got {len(copies)}")
         if copies is not None and any(c is not None for c in copies):
             some = [c for c in copies if c is not None]
             _check_tensors(some, {torch.bfloat16}, self.device, "copies")
