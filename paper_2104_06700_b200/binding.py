@@ -317,15 +317,14 @@ class AdamwList:
         self._keep = None
 
     def refresh(self, grads, params=None, copies=None) -> None:
-        """Names (and checks) what may lie elsewhere at every step."""
-        fields = self._fields
-        self._keep = grads      # what a caller made for this step alone has to live until the launch
+        """Names (and checks) what may lie elsewhere at every step.  If it is refused the list stays as it was."""
+        fields, types_now = list(self._fields), list(self._types)
         for at, type_at, name, tensors in ((2, 9, "grads", grads), (1, 8, "params", params)):
             if tensors is not None:
                 types = _check_tensors(tensors, _FLOAT_SET, self.device, name)
-                if types != self._types[at - 1]:
+                if types != types_now[at - 1]:
                     fields[type_at] = array("i", map(_TYPE_CODES.__getitem__, types))
-                    self._types[at - 1] = types
+                    types_now[at - 1] = types
                 _check_sizes(tensors, self._numbers, name)
                 fields[at] = _pointers(tensors)
         if copies is not None and len(copies) != self.count:
@@ -338,6 +337,8 @@ class AdamwList:
         else:
             fields[6] = None
         self.struct = struct.pack("q12Q", self.count, *[0 if f is None else f.buffer_info()[0] for f in fields])
+        self._fields, self._types = fields, types_now    # the arrays that the struct points to
+        self._keep = grads      # what a caller made for this step alone has to live until the launch
 
 
 def adamw_workspace(device) -> torch.Tensor:

@@ -1,4 +1,6 @@
-"""Lists of tensors for the AdamW calls (binding.AdamwList): what they refuse, without a GPU."""
+"""Lists of tensors for the AdamW calls (binding.AdamwList): what they refuse, and that a refusal leaves them whole, without a GPU."""
+import struct
+
 import pytest
 import torch
 
@@ -14,6 +16,39 @@ def on_cpu(monkeypatch):
             raise TypeError(name)
         return types
     monkeypatch.setattr(binding, "_check_tensors", check)
+
+
+def arrays_are_its_own(a, count):
+    """What the struct points to are the list's arrays, with as many entries as tensors."""
+    got = struct.unpack("q12Q", a.struct)
+    assert got[0] == count
+    for where, field in zip(got[1:], a._fields):
+        assert where == (0 if field is None else field.buffer_info()[0])
+        assert field is None or len(field) == count
+
+
+def test_a_refused_refresh_leaves_the_list_as_it_was(on_cpu):
+    n = [5, 300, 7]
+    f = lambda dtype=torch.float32: [torch.zeros(k, dtype=dtype) for k in n]  # noqa: E731
+    grads, params, copies = f(), f(), f(torch.bfloat16)
+    a = binding.AdamwList(grads, params, f(), f(), [torch.zeros((), dtype=torch.int64) for _ in n], copies=copies)
+    arrays_are_its_own(a, 3)
+    was, fields = a.struct, list(a._fields)
+    short = [torch.zeros(k - 1) for k in n]
+    for wrong in ((short, params, copies), (f(torch.bfloat16), short, copies), (f(torch.bfloat16), f(torch.bfloat16), short),
+                  (grads, params, [c[1:] for c in copies]), (f(torch.float64), params, copies), (grads[:2], params, copies),
+                  (grads, params[:2], copies), (grads, params, copies[:2])):
+        with pytest.raises((ValueError, TypeError)):
+            a.refresh(*wrong)
+        assert a.struct == was and all(x is y for x, y in zip(a._fields, fields))
+        arrays_are_its_own(a, 3)
+    moved = f(torch.bfloat16)
+    a.refresh(moved, params, copies)
+    arrays_are_its_own(a, 3)
+    assert list(a._fields[2]) == [t.data_ptr() for t in moved] and list(a._fields[9]) == [binding.DG_BF16] * 3
+    a.refresh(grads, params, None)
+    arrays_are_its_own(a, 3)
+    assert a._fields[6] is None and list(a._fields[9]) == [binding.DG_F32] * 3
 
 
 def test_columns_of_another_length_are_refused(on_cpu):
