@@ -351,11 +351,17 @@ def _workspace_ptr(workspace):
     return _dev_ptr(workspace, torch.uint8, "workspace")
 
 
+def _list_struct(tensors: AdamwList) -> bytes:
+    if tensors.count and tensors.device != _device():
+        raise ValueError(f"the current device is cuda:{_device()}, but the list's tensors are on cuda:{tensors.device}")
+    return tensors.struct
+
+
 def dg_grad_norm(tensors: AdamwList, max_norm: float, workspace: torch.Tensor, result: torch.Tensor, stream=None) -> torch.Tensor:
     """Wraps ``dg_grad_norm``: result (2 fp32) = (norm of all gradients, min(1, max_norm / (norm + 1e-6)))."""
     _has(result, 2, "result")
     _on_current_device(result=result, workspace=workspace)
-    _check(lib().dg_grad_norm(tensors.struct, max_norm, _workspace_ptr(workspace), _dev_ptr(result, torch.float32, "result"),
+    _check(lib().dg_grad_norm(_list_struct(tensors), max_norm, _workspace_ptr(workspace), _dev_ptr(result, torch.float32, "result"),
                               _stream(stream)))
     return result
 
@@ -365,7 +371,7 @@ def dg_adamw_step(tensors: AdamwList, lr: float, beta1: float, beta2: float, eps
     """Wraps ``dg_adamw_step``: updates the tensors, their states and their steps in place."""
     _has(grad_factor, 1, "grad_factor")
     _on_current_device(grad_factor=grad_factor, workspace=workspace)
-    _check(lib().dg_adamw_step(tensors.struct, lr, beta1, beta2, eps, weight_decay,
+    _check(lib().dg_adamw_step(_list_struct(tensors), lr, beta1, beta2, eps, weight_decay,
                                _dev_ptr(grad_factor, torch.float32, "grad_factor"), seed & 0xffffffffffffffff,
                                _workspace_ptr(workspace), _stream(stream)))
 

@@ -562,6 +562,9 @@ static dg_status_t norm_args(const Graph* g, const void* X, dg_type_t x_type, in
                              const float* weight, const float* bias, const float* stats, dg_act_t act, dg_type_t y_type,
                              NormArgs* a) {
   if (!g) return invalid("graph handle is NULL");
+  int device = -1;  // the batch's offsets lie on the handle's
+  if (cudaError_t e = cudaGetDevice(&device)) return cuda_fail(e, "cudaGetDevice");
+  if (device != g->device) return invalid("the graph handle belongs to another device than the current one");
   if (F < 1 || F > (1 << 20)) return invalid("F must be from 1 to 2^20");
   if (groups < 1 || groups > F || F % groups != 0) return invalid("groups must divide F");
   if ((x_type != DG_F32 && x_type != DG_BF16) || (y_type != DG_F32 && y_type != DG_BF16))
