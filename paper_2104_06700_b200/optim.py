@@ -31,6 +31,15 @@ class _Table:
         self.list = binding.AdamwList(grads, self.targets, *columns, self.copies, ids)
 
 
+def _check_options(options) -> None:
+    if options["state_bits"] not in (8, 32):
+        raise ValueError(f"state_bits must be 8 or 32, got {options['state_bits']}")
+    if not options["lr"] >= 0 or not options["eps"] >= 0 or not options["weight_decay"] >= 0:
+        raise ValueError("lr, eps and weight_decay must not be negative")
+    if len(options["betas"]) != 2 or not all(0 <= b < 1 for b in options["betas"]):
+        raise ValueError(f"betas must be in [0, 1), got {options['betas']}")
+
+
 class AdamW(torch.optim.Optimizer):
     """torch.optim.AdamW's update (decoupled weight decay) for fp32 and bf16 parameters on one GPU.
 
@@ -49,21 +58,18 @@ class AdamW(torch.optim.Optimizer):
     def __init__(self, params, lr: float = 1e-3, betas=(0.9, 0.999), eps: float = 1e-8, weight_decay: float = 1e-2,
                  state_bits: int = 32, min_8bit_size: int = 4096, master_weights: bool = False,
                  max_norm: Optional[float] = None, seed: int = 0):
-        if state_bits not in (8, 32):
-            raise ValueError(f"state_bits must be 8 or 32, got {state_bits}")
         if max_norm is not None and not max_norm > 0:
             raise ValueError(f"max_norm must be positive, got {max_norm}")
-        if not lr >= 0 or not eps >= 0 or not weight_decay >= 0:
-            raise ValueError("lr, eps and weight_decay must not be negative")
-        if len(betas) != 2 or not all(0 <= b < 1 for b in betas):
-            raise ValueError(f"betas must be in [0, 1), got {betas}")
+        defaults = dict(lr=lr, betas=betas, eps=eps, weight_decay=weight_decay, state_bits=state_bits,
+                        min_8bit_size=min_8bit_size, master_weights=master_weights, seed=seed)
+        _check_options(defaults)
         self.max_norm, self.grad_norm = max_norm, None
         self._workspace = self._result = None
         self._tables, self._known_state, self._standing = {}, None, False
-        super().__init__(params, dict(lr=lr, betas=betas, eps=eps, weight_decay=weight_decay, state_bits=state_bits,
-                                      min_8bit_size=min_8bit_size, master_weights=master_weights, seed=seed))
+        super().__init__(params, defaults)
 
     def add_param_group(self, group) -> None:
+        _check_options({**self.defaults, **group})
         super().add_param_group(group)
         params = self.param_groups[-1]["params"]
         if len(set(params)) != len(params):
