@@ -309,14 +309,18 @@ dg_status_t dg_cross_entropy_bwd(dg_graph_t g, const float* logits, int32_t C, c
  *   exp_avg, exp_avg_sq  state_bits = 32: m and v, fp32.  state_bits = 8: m and sqrt(v), e4m3 bytes, times the scales; rounded
  *               up or down at random, a sqrt(v) > 0 never to 0.  A number that is not finite becomes NaN and leaves the rest
  *               of its block alone.  What is rounded comes of the formulas operation by operation, each rounded to fp32, so that
- *               other fp32 arithmetic arrives at the same codes and scales
+ *               other fp32 arithmetic arrives at the same codes and scales: y = min(|x| * (1 / scale), 448), and the code is that of
+ *               y + (r + 1/2) / 2^16 steps rounded down, where a step is e4m3's at y and r 16 random bits (the lower half of the
+ *               number's 32 for m, the upper one for sqrt(v)); below 2^-6, y is first rounded to a multiple of 2^-29
  *   scales      state_bits = 8: 2 fp32 for every 256 numbers begun (of m, of sqrt(v)), 8-byte aligned; else NULL, and the array
- *               itself may be NULL where all are
+ *               itself may be NULL where all are.  The new ones are the largest finite |x| of the block times fp32's 1 / 448 (not
+ *               divided by 448, which may differ in the last bit), at least 2^-126
  *   step        steps taken so far; read, then increased by 1 by the call (one number for each tensor)
  *   id          what the random bits of the tensor go by, beside the seed; the array may be NULL: i
  * All zeros are the states of a new tensor.  Tensors must not overlap.
  * dg_adamw_step: `grad_factor` is a device fp32 or NULL (1): result + 1 of dg_grad_norm.  The random bits of a rounding are a hash
- * of (seed, steps so far, id, place): the same call on the same data gives the same bits.  lr and the others are taken by
+ * of (seed, steps so far, id, place): the same call on the same data gives the same bits.  With h the 32-bit hash lowbias32 they are
+ * h(low(place) + h(key ^ high(place))), key = h(h(h(h(low(seed) + 0x9e3779b9) ^ high(seed)) + low(steps)) ^ id).  lr and the others are taken by
  * value: a captured call repeats them, while the steps go on counting.
  * dg_grad_norm: result[0] = the 2-norm of all gradients (of a list only grad, grad_type and numbers are looked at), added in 64
  * bits in a fixed order, result[1] = min(1, max_norm / (result[0] + 1e-6)): clipping by the norm.
