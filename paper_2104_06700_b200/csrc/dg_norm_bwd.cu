@@ -93,7 +93,6 @@ __global__ void __launch_bounds__(kNormThreads, kPieceBlocks)
       }
       all = Sums<ACT, VEC>{};
     };
-    int32_t steps = 0;
     auto step = [&](auto once) {
       constexpr bool kOnce = decltype(once)::value;
       Channels<VEC> v[kRows], d[kRows];
@@ -106,11 +105,18 @@ __global__ void __launch_bounds__(kNormThreads, kPieceBlocks)
 #pragma unroll
       for (int u = 0; u < kRows; ++u) some.add(v[u], d[u], f);
       all.add(some);
-      if (++steps % kStretch == 0) close();
       rows -= kRows, x += kRows * pace, dy += kRows * pace;
     };
-    while (rows >= kRows + sh.kept) step(std::true_type());
-    while (rows >= kRows) step(std::false_type());
+    while (rows >= kRows + sh.kept) {
+#pragma unroll 1
+      for (int q = 0; q < kStretch && rows >= kRows + sh.kept; ++q) step(std::true_type());
+      close();
+    }
+    while (rows >= kRows) {
+#pragma unroll 1
+      for (int q = 0; q < kStretch && rows >= kRows; ++q) step(std::false_type());
+      close();
+    }
     for (; rows > 0; --rows, x += pace, dy += pace) all.add(load_channels<X, VEC, false>(x), load_channels<Y, VEC, false>(dy), f);
     close();
   }
