@@ -221,9 +221,9 @@ dg_status_t dg_layer_bwd(dg_graph_t g, const float* dOut, const float* out, int3
  *   count    number of graphs; 0: one graph of all n vertices again (the state of a new handle; offsets is not read)
  *   offsets  HOST, count + 1 entries, not decreasing, from 0 to at most n: graph b has the vertices offsets[b] ..
  *            offsets[b + 1] - 1.  A graph may be empty; vertices from offsets[count] on belong to none (padding).
- * Only the group norm below looks at them.  The handle keeps a copy on the device.  Waits for the whole device, like a
- * change of "rows_per_block": CUDA graphs captured before it must not be launched afterwards.  If it fails the handle is
- * as it was.  dg_graph_reorder does not carry the graphs over: it mixes their vertices.
+ * Only the group norm below looks at them.  The handle keeps a copy on the device.  Waits for the whole device (count = 0 need
+ * not), like a change of "rows_per_block": CUDA graphs captured before it must not be launched afterwards.  If it fails the handle
+ * is as it was.  dg_graph_reorder does not carry the graphs over: it mixes their vertices.
  */
 dg_status_t dg_graph_set_batch(dg_graph_t g, int64_t count, const int64_t* offsets);
 
@@ -241,9 +241,11 @@ dg_status_t dg_graph_set_batch(dg_graph_t g, int64_t count, const int64_t* offse
  *   weight, bias  device, F fp32 each, or NULL: 1 and 0
  *   stats    device, graphs * groups * 2 fp32, 8-byte aligned; written by fwd, read by bwd
  *   dX, dweight, dbias  each may be NULL and is not formed then
- * Statistics and sums are fp32 or wider and always added in the same order; a result is rounded to its type once.  Rows that belong to no
- * graph are neither read nor written.  Results must not overlap inputs.  The ReLU's gradient is that of z > 0 with the
- * sign of z taken in 64 bits where fp32 leaves it open.  graphs * groups < 2^31.  Asynchronous on `stream`.
+ * Statistics and sums are fp32 or wider (a thread's fp32 sums go over 128 rows at most) and always added in the same order; a
+ * result is rounded to its type once.  A number that is not finite reaches no other group of its graph and no other graph, except
+ * through dweight and dbias, which are sums over all graphs.  Rows that belong to no graph are neither read nor written.  Results
+ * must not overlap inputs.  The handle has to belong to the current device.  The ReLU's gradient is that of z > 0 with the sign of z
+ * taken in 64 bits where fp32 leaves it open.  graphs * groups < 2^31.  Asynchronous on `stream`.
  */
 typedef enum { DG_F32 = 0, DG_BF16 = 1 } dg_type_t;
 typedef enum { DG_ACT_NONE = 0, DG_ACT_RELU = 1, DG_ACT_SILU = 2 } dg_act_t;
@@ -320,8 +322,8 @@ dg_status_t dg_cross_entropy_bwd(dg_graph_t g, const float* logits, int32_t C, c
  * All zeros are the states of a new tensor.  Tensors must not overlap.
  * dg_adamw_step: `grad_factor` is a device fp32 or NULL (1): result + 1 of dg_grad_norm.  The random bits of a rounding are a hash
  * of (seed, steps so far, id, place): the same call on the same data gives the same bits.  With h the 32-bit hash lowbias32 they are
- * h(low(place) + h(key ^ high(place))), key = h(h(h(h(low(seed) + 0x9e3779b9) ^ high(seed)) + low(steps)) ^ id).  lr and the others are taken by
- * value: a captured call repeats them, while the steps go on counting.
+ * h(low(place) + h(key ^ high(place))), key = h(h(h(h(low(seed) + 0x9e3779b9) ^ high(seed)) + low(steps)) ^ id).  lr and the others
+ * are taken by value: a captured call repeats them, while the steps go on counting.
  * dg_grad_norm: result[0] = the 2-norm of all gradients (of a list only grad, grad_type and numbers are looked at), added in 64
  * bits in a fixed order, result[1] = min(1, max_norm / (result[0] + 1e-6)): clipping by the norm.
  *   workspace   device, DG_ADAMW_WORKSPACE_BYTES, 256-byte aligned, cleared to 0 before its first use; calls leave it ready for

@@ -19,12 +19,13 @@ namespace {
 constexpr int kThreads = 256;
 constexpr int kWarps = kThreads / 32;
 // Blocks of an SM.  Numbers in 32 bits: two, whose 128 registers a thread hold a task's first block while the powers of beta
-// are on their way (245 M numbers, clipped: 1204 us, three blocks 1260).  In 8 bits arithmetic counts, and more warps hide it:
-// four at 64 registers, of which up to 19 are spilled (245 M numbers: 699 us; three blocks 760).
+// are on their way (245 M numbers, clipped: 1205 us, three blocks 1396).  In 8 bits arithmetic counts, and more warps hide it:
+// four at 64 registers, of which up to 19 are spilled (245 M numbers, launches with pauses between them: 686 us, three blocks 744;
+// without pauses, at the clocks that leaves, 711 - 752).
 constexpr int blocks_per_sm(bool eight) { return eight ? 4 : 2; }
 constexpr int kNumbers = 256;                       // of a warp's task: 8 a lane, and one scale
-// 256 numbers each, of a warp's task.  8-bit states: see step_kind (245 M numbers 718 -> 705 us against four, 120 tensors of
-// 37 M 137 -> 130).
+// 256 numbers each, of a warp's task.  8-bit states: see step_kind (245 M numbers, with pauses: 686 us, 706 with four; 120 tensors of
+// 37 M 136, 140).
 constexpr int kBlocksPerTask = 4, kMostBlocks = 16;
 constexpr int kNormNumbers = 2048;                  // of a warp's task of the norm
 constexpr int kNormBlocks = 148 * 4;

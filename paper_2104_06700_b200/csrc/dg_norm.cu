@@ -553,9 +553,9 @@ GraphPlan graph_plan(const Graph* g, const NormArgs& a, int vec, int x_bytes, in
     return plan;
   }
   // Many: those of more than eight times what a block keeps in narrow tiles, the others as wide as an average graph leaves
-  // threads with rows.  2048 graphs of 1 to 2500 rows of 128, forward / backward: 32 / 56 us; narrow from twice what a block
-  // keeps on 33 / 58, from once 38 / 65; the long ones by clusters 43 / 74, in pieces as the long graphs' kernels take them
-  // 52 / 107.
+  // threads with rows.  2048 graphs of 1 to 2500 rows of 128, forward / backward, from a cold L2: 39 / 52 us; narrow from twice what
+  // a block keeps on 39 / 64, from once 49 / 76; in pieces as the long graphs' kernels take them 64 / 123.  (The long ones by
+  // clusters, when this was chosen: 43 / 74 where it was 33 / 58.)
   first = shape(narrow(64));
   if (longest > 16 * kept(first)) return none;
   across = first.across;
